@@ -134,7 +134,9 @@ int32_t crf_abi_version(void);
  * (head_dim+4), 35 MB at head_dim 128), K-split LoRA partials and, when max_lora_rank > 0, the down projection's
  * adapter sums formed inside the gate/up projection (4 x 2 x 256 x 16 floats
  * per compute unit, 32 MiB on 256 CUs, plus one int per gate/up tile), and 2 KiB
- * of arrival counters.  All of
+ * of arrival counters.  An fp32 context holds 64 MiB of partials for
+ * crf_paged_attention (a bf16 one uses the K-parts' scratch), and every context
+ * 21 KiB of counters for the operators over a page pool.  All of
  * it is freed by crf_context_destroy.  On success *out
  * receives the context.  Errors: INVALID_ARG (null), UNSUPPORTED (see
  * crf_validate_dims), HIP (allocation failed). */
@@ -300,9 +302,177 @@ crf_status crf_layer_drift_noalloc(const crf_model_dims *dims, const crf_lora_la
                                    const float *sensitivity, int32_t per_layer_only, float *drift_out,
                                    float *risk_out, float *sq_partial_out, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Many sequences in one cache: operators of a server that keeps the caches of
+ * many sequences, each perhaps of another adapter version, in one pool of pages.
+ *
+ * They take the pool's layout and the head layout of crf_kv_cache and of the
+ * context's dims, in both storage types.  Everything about a sequence (its
+ * length, its new tokens, its pages) is read on the device, so a captured call
+ * follows the values at each replay; the host gives bounds.  Conventions as
+ * above: asynchronous on `stream`, nothing allocated, checks on the host before
+ * any launch, the kernels' own checks reported by crf_context_device_errors.
+ * The current device must be the context's (else INVALID_ARG).  Calls on one
+ * context share its workspace: they run one after the other, on one stream or
+ * ordered by the caller, captured ones and their replays too. */
+
+/* The pages of all layers.  Element (layer, page, kv_head, slot, e) of a pool is
+ * where crf_kv_cache has it; a layer of a pool may pass 2 GiB.  Pools 16-byte
+ * aligned, strides (elements) multiples of 8. */
+typedef struct {
+  void *k_pool, *v_pool;
+  int64_t layer_stride, page_stride;
+  int32_t n_pages, page_size;
+} crf_page_pool;
+
+/* The new tokens of many sequences.  Rows row_start[s] .. row_start[s+1]-1 of the
+ * call's tensors are the last tokens of sequence s, which has length[s] tokens
+ * with them: row r sits at position length[s] - row_start[s+1] + r, in page
+ * block_tables[s][position / page_size].  A sequence may have no new token.
+ * Rows past row_start[n_seqs] belong to nobody and are left as they are.
+ * row_start [n_seqs+1] (not descending), length [n_seqs] and block_tables
+ * [n_seqs][table_stride] are DEVICE int32.  A sequence whose rows or length
+ * contradict the bounds below raises error bit 1 and has no new tokens. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_rows;       /* rows of the call's tensors                            */
+  int32_t max_new;      /* no sequence has more new tokens (0: n_rows)           */
+  int32_t max_pages;    /* no sequence has more pages                            */
+  int64_t table_stride; /* entries between the rows of block_tables              */
+  const int32_t *row_start, *length, *block_tables;
+} crf_seq_batch;
+
+/* Rotary positions: which elements of a head pair up, how much of the head
+ * rotates (the rest passes) and by what angle.  freq[i]: radians per position of
+ * pair i; mscale: factor on every cosine and sine.  Made by crf_rope_init, or by
+ * the caller for frequencies of its own. */
+enum { CRF_ROPE_HALF = 0,         /* pairs (i, i + rotary_dim/2), as the windows use */
+       CRF_ROPE_INTERLEAVED = 1   /* pairs (2i, 2i + 1)                              */ };
+typedef struct {
+  int32_t layout, rotary_dim;
+  float mscale;
+  double freq[64];
+} crf_rope;
+
+/* Scaling of the frequencies f_i = theta^(-2i/rotary_dim) for contexts longer
+ * than the trained ones:
+ *   NONE    f_i;
+ *   LINEAR  f_i / factor (positions interpolated);
+ *   BASE    of theta * factor^(rotary_dim / (rotary_dim - 2)) instead of theta;
+ *   PARTS   f_i (g_i + (1 - g_i) / factor), g_i the turns f_i original_len / 2 pi of
+ *           a pair over the trained length, put on [0, 1] between low_turns and
+ *           high_turns (0: 1 and 32).
+ * mscale 0: 0.1 ln(factor) + 1 for PARTS with factor > 1, else 1. */
+enum { CRF_ROPE_NONE = 0, CRF_ROPE_LINEAR, CRF_ROPE_BASE, CRF_ROPE_PARTS };
+typedef struct {
+  int32_t kind;
+  double factor;
+  double original_len;
+  double low_turns, high_turns;
+  double mscale;
+} crf_rope_scaling;
+
+/* Host only.  scaling NULL: none.  Errors: INVALID_ARG (NULL, unknown layout or
+ * scaling), UNSUPPORTED (rotary_dim no multiple of 16 in [0, 128]), SHAPE
+ * (theta, factor, mscale, original_len or turns out of range). */
+crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, double theta,
+                         const crf_rope_scaling *scaling);
+
+/* Rotates q into q_out, and appends the new tokens to the cache: k rotated, v as
+ * it is, into layer `layer` of the pages at the tokens' positions (which the
+ * block tables must already cover, see crf_pages_extend).
+ *   q [n_rows][n_q_heads][head_dim], k, v [n_rows][n_kv_heads][head_dim], rows
+ *   *_stride elements apart (slices of one fused projection), 16-byte aligned;
+ *   q_out may be q; both NULL: keys and values only.
+ *   positions: DEVICE int32 [n_rows], rotary positions other than the cache's
+ *   (NULL: the cache's).  Angles are reduced in 64 bits at every position.
+ * A token on a page out of range raises error bit 0 and is not appended (its q is
+ * still rotated).
+ * Errors: INVALID_ARG, SHAPE, RANGE (layer), UNSUPPORTED (rotary_dim above
+ * head_dim or no multiple of 16, more than 2^30 tokens a table or rows x heads). */
+crf_status crf_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq_batch *batch,
+                           const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride,
+                           const crf_page_pool *pool, int32_t layer, void *stream);
+
+/* Softmax attention of every new token over its sequence's pages in layer
+ * `layer`: a row at position p sees the keys j <= p, and with window > 0 only
+ * those with j > p - window; query head i reads K/V head i / (n_q_heads/n_kv_heads).
+ *   q, out [n_rows][n_q_heads][head_dim] as above; out may be q.
+ *   scale: of the scores (0: 1/sqrt(head_dim)).
+ *   lse (nullable): fp32 [n_rows][n_q_heads], the natural logarithm of each row's
+ *   sum of exponentials, by which results over parts of a cache can be joined.
+ * Keys on pages out of range are seen by nobody (error bit 0); a row that sees no
+ * key gets zeros and lse -inf.  What lies in slots past a sequence's length, or in
+ * keys that a row does not see, has no influence on it, numbers or not.  The
+ * result is the same to the bit for every call with the same inputs.
+ * Errors: INVALID_ARG, SHAPE (negative or non-finite scale, negative window,
+ * strides), RANGE (layer), UNSUPPORTED (as crf_rope_append). */
+crf_status crf_paged_attention(crf_context *ctx, const crf_seq_batch *batch, const void *q, int64_t q_stride,
+                               const crf_page_pool *pool, int32_t layer, float scale, int32_t window, void *out,
+                               int64_t out_stride, float *lse, void *stream);
+
+/* Copies pages src[i] of `from` to pages dst[i] of `to` for i < n, in h layers
+ * from from_l0 and to_l0 on: a window's layers saved before a refresh overwrites
+ * them, or a cache duplicated for another adapter version.  src, dst: DEVICE
+ * int32.  The dst pages must differ from each other and, within one pool, from
+ * every src page; else what they hold is one of the sources, in pieces.  A page
+ * out of range raises error bit 0 and is skipped.
+ * Errors: INVALID_ARG, SHAPE (page sizes differ), RANGE (layers), UNSUPPORTED. */
+crf_status crf_pages_copy(crf_context *ctx, const crf_page_pool *from, int32_t from_l0, const crf_page_pool *to,
+                          int32_t to_l0, int32_t h, int32_t n, const int32_t *src, const int32_t *dst, void *stream);
+
+/* Who holds which pages, all DEVICE int32: refs [n_pages], how many sequences
+ * hold each page (0: free); block_tables [n_seqs][table_stride], of which a
+ * sequence's first ceil(length / page_size) entries are in use; lengths [n_seqs]
+ * (0: no sequence).  At most 2^19 pages, 4096 sequences and 2^30 tokens a
+ * sequence (else UNSUPPORTED).  Free pages are always taken lowest first, in the
+ * order of the sequences (or forks) that need them. */
+typedef struct {
+  int32_t *refs, *block_tables, *lengths;
+  int64_t table_stride;
+  int32_t n_pages, page_size, n_seqs, max_pages;
+} crf_page_map;
+
+/* Makes children[i], which must be empty, a copy of parents[i] for i < n <= 4096
+ * (DEVICE int32): it shares the parent's full pages and gets a copy of a page
+ * that the parent has begun, in every layer of the context's dims, so that both
+ * can be extended.  Parents are taken as they are before the call.  A fork that
+ * names a sequence out of range, a child that is not empty or a child that an
+ * earlier fork of the call names is skipped (error bit 1), and one for whose page
+ * no free page is left (error bit 2); its child stays empty.
+ * Errors: INVALID_ARG, SHAPE (map and pool differ), UNSUPPORTED. */
+crf_status crf_pages_fork(crf_context *ctx, const crf_page_pool *pool, const crf_page_map *map, int32_t n,
+                          const int32_t *parents, const int32_t *children, void *stream);
+
+/* Makes every sequence n_new[s] tokens longer (DEVICE int32 [n_seqs]), with the
+ * pages that this takes.  A sequence for which n_new is negative or which would
+ * pass max_pages keeps its length (error bit 1); once too few pages are free for
+ * one, it and every later one that needs any keep theirs (error bit 2).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED. */
+crf_status crf_pages_extend(crf_context *ctx, const crf_page_map *map, const int32_t *n_new, void *stream);
+
+/* Ends n sequences (DEVICE int32): their pages are held by one fewer, their
+ * length is 0, their table rows are left.  A sequence that is empty or named
+ * twice is freed once; one out of range, or a page that nobody holds, raises
+ * error bit 1.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED. */
+crf_status crf_pages_free(crf_context *ctx, const crf_page_map *map, int32_t n, const int32_t *seqs, void *stream);
+
+/* Moves the pages in use to the front of the pool, in every layer: with L of
+ * them, the k-th at or past L goes to the k-th free one below L.  map_out, which
+ * may be map or any of its arrays, receives the new counts, tables and lengths;
+ * remap [n_pages] the new place of every page (-1: it was free); counts [2] L and
+ * the number of pages moved (all DEVICE int32).  The pages moved keep their bytes
+ * in their old places, so readers through the old map are right until those are
+ * used again.  A table entry that names no page in use becomes -1 (error bit 0).
+ * Errors: INVALID_ARG, SHAPE (maps or pool differ), UNSUPPORTED, WORKSPACE. */
+crf_status crf_pages_compact(crf_context *ctx, const crf_page_pool *pool, const crf_page_map *map,
+                             const crf_page_map *map_out, int32_t *remap, int32_t *counts, void *stream);
+
 /* Device-side error flags raised by kernels' own bounds checks since the last
- * call (bit 0: a block table entry outside [0, n_pages)).  Synchronises the
- * device, then clears the flags. */
+ * call (bit 0: a block table entry outside [0, n_pages); bit 1: a sequence of a
+ * batch or page map that contradicts it; bit 2: too few free pages).
+ * Synchronises the device, then clears the flags. */
 crf_status crf_context_device_errors(crf_context *ctx, int32_t *flags_out);
 
 /* Optional per-kernel-class event timing.  While enabled, each launch is

@@ -62,6 +62,34 @@ class WindowItem(ctypes.Structure):
                 ("hidden_out", ctypes.c_void_p)]
 
 
+class PagePool(ctypes.Structure):
+    _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
+                ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class SeqBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int64),
+                ("row_start", ctypes.c_void_p), ("length", ctypes.c_void_p), ("block_tables", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("mscale", ctypes.c_float),
+                ("freq", ctypes.c_double * 64)]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double), ("mscale", ctypes.c_double)]
+
+
+class PageMap(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("block_tables", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
 # ----------------------------------------------------------------------------- loading
 
 _LIB: Optional[ctypes.CDLL] = None
@@ -70,7 +98,9 @@ EXPORTS = ("crf_status_string", "crf_abi_version", "crf_context_create", "crf_co
            "crf_validate_dims", "crf_validate_window", "crf_recompute_window", "crf_recompute_window_batched",
            "crf_layer_drift", "crf_context_device_errors", "crf_context_set_timing", "crf_context_set_timing_classes",
            "crf_context_read_timing",
-           "crf_device_info", "crf_decode_logits", "crf_layer_drift_noalloc")
+           "crf_device_info", "crf_decode_logits", "crf_layer_drift_noalloc", "crf_rope_init", "crf_rope_append",
+           "crf_paged_attention", "crf_pages_copy", "crf_pages_fork", "crf_pages_extend", "crf_pages_free",
+           "crf_pages_compact")
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -119,6 +149,18 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                       I32, VP, VP]
     lib.crf_device_info.restype = I32
     lib.crf_device_info.argtypes = [I32, P(I32), P(I32), ctypes.c_char_p, I32]
+    I64 = ctypes.c_int64
+    for name, args in (
+            ("rope_init", [P(Rope), I32, I32, ctypes.c_double, P(RopeScaling)]),
+            ("rope_append", [VP, P(Rope), P(SeqBatch), VP, VP, I64, VP, I64, VP, I64, VP, I64, P(PagePool), I32, VP]),
+            ("paged_attention", [VP, P(SeqBatch), VP, I64, P(PagePool), I32, ctypes.c_float, I32, VP, I64, VP, VP]),
+            ("pages_copy", [VP, P(PagePool), I32, P(PagePool), I32, I32, I32, VP, VP, VP]),
+            ("pages_fork", [VP, P(PagePool), P(PageMap), I32, VP, VP, VP]),
+            ("pages_extend", [VP, P(PageMap), VP, VP]),
+            ("pages_free", [VP, P(PageMap), I32, VP, VP]),
+            ("pages_compact", [VP, P(PagePool), P(PageMap), P(PageMap), VP, VP, VP])):
+        fn = getattr(lib, "crf_" + name)
+        fn.restype, fn.argtypes = I32, args
     _LIB = lib
     return lib
 
@@ -208,6 +250,8 @@ class Context:
         _err(self.lib, None, self.lib.crf_context_create(ctypes.byref(dims), int(max_tokens), int(max_lora_rank),
                                                           ctypes.byref(h)))
         self.handle = h
+        import torch
+        self.device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "handle", None) and self.handle.value:
@@ -339,3 +383,200 @@ def layer_drift_noalloc(dims: ModelDims, current: ctypes.Array, versions: Sequen
                                      1 if per_layer_only else 0, _ptr(drift_out), _ptr(risk_out),
                                      _ptr(sq_partial_out), _stream(stream))
     _err(lib, None, st)
+
+
+# ----------------------------------------------------------------------------- many sequences in one cache
+
+ROPE_LAYOUTS = ("half", "interleaved")
+ROPE_SCALINGS = ("none", "linear", "base", "parts")
+
+
+def _same_device(*tensors) -> int:
+    """The device of a descriptor's tensors (-1: host memory, which no call takes)."""
+    dev = tensors[0].get_device()
+    if any(t.get_device() != dev for t in tensors):
+        raise CrfError(1, "tensors of one descriptor lie on different devices")
+    return dev
+
+
+def _check_device(ctx: Context, *parts):
+    """Tensors and descriptors of a call lie on the context's device."""
+    for t in parts:
+        if t is None:
+            continue
+        dev = t.device if isinstance(t, ctypes.Structure) else t.get_device()
+        if dev != ctx.device:
+            raise CrfError(1, f"a tensor on {'the host' if dev < 0 else f'device {dev}'}, the context on device {ctx.device}")
+
+
+def _int32(t, n: Optional[int], name: str):
+    """A contiguous int32 device vector (of n values)."""
+    import torch
+    if t.dtype is not torch.int32 or t.dim() != 1 or (t.numel() > 1 and t.stride(0) != 1) or \
+            (n is not None and t.numel() != n):
+        raise CrfError(2, f"{name} must be a contiguous int32 vector" + (f" of {n}" if n is not None else ""))
+    return t
+
+
+def _tables(t):
+    import torch
+    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise CrfError(2, "block tables must be int32 [sequences, entries], entries contiguous")
+    return t
+
+
+def _head_rows(ctx: Context, t, n_rows: int, heads: int, name: str):
+    """Pointer and row stride of [rows, heads, head_dim] or [rows, heads * head_dim] whose rows are contiguous."""
+    import torch
+    d = ctx.dims
+    want = torch.bfloat16 if d.dtype == CRF_BF16 else torch.float32
+    if t.dtype is not want:
+        raise CrfError(1, f"{name} is {t.dtype}, the context's storage type {want}")
+    shape, stride = t.shape, t.stride()
+    ok = shape[0] == n_rows and stride[-1] == 1
+    if len(shape) == 3:
+        ok = ok and shape[1] == heads and shape[2] == d.head_dim and (heads == 1 or stride[1] == d.head_dim)
+    else:
+        ok = ok and len(shape) == 2 and shape[1] == heads * d.head_dim
+    if not ok:
+        raise CrfError(2, f"{name} {tuple(shape)} (strides {stride}) is not {n_rows} rows of {heads} heads of "
+                          f"{d.head_dim}")
+    return t.data_ptr(), stride[0] if n_rows > 1 else heads * d.head_dim
+
+
+def page_pool(k_pool, v_pool, page_size: int) -> PagePool:
+    """k_pool, v_pool: [n_layers, n_pages, n_kv_heads, page_size, head_dim] device tensors."""
+    if k_pool.dtype is not v_pool.dtype or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() or \
+            k_pool.dim() != 5 or not k_pool[0, 0].is_contiguous() or k_pool.shape[3] != page_size:
+        raise CrfError(2, "pools must be two like tensors [layers, pages, kv heads, page_size, head_dim], pages contiguous")
+    p = PagePool(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), k_pool.stride(1), k_pool.shape[1], page_size)
+    p.tensors, p.device = (k_pool, v_pool), _same_device(k_pool, v_pool)
+    return p
+
+
+def _check_pool(ctx: Context, pool: PagePool, layers: int):
+    """The pool's storage type and heads are the context's, and it has that many layers."""
+    import torch
+    k, d = pool.tensors[0], ctx.dims
+    if k.dtype is not (torch.bfloat16 if d.dtype == CRF_BF16 else torch.float32):
+        raise CrfError(1, f"the pool is {k.dtype}, the context's storage type differs")
+    if k.shape[2] != d.n_kv_heads or k.shape[4] != d.head_dim:
+        raise CrfError(2, f"the pool has {k.shape[2]} heads of {k.shape[4]}, the context {d.n_kv_heads} of {d.head_dim}")
+    if not 0 <= layers <= k.shape[0]:
+        raise CrfError(3, f"{layers} layers of a pool of {k.shape[0]}")
+
+
+def seq_batch(row_start, length, block_tables, n_rows: int, max_new: int = 0) -> SeqBatch:
+    """row_start [S + 1], length [S], block_tables [S, pages]: int32 device tensors; n_rows: rows of the
+    calls' tensors; max_new: the most new tokens of a sequence (0: n_rows)."""
+    t = _tables(block_tables)
+    n = t.shape[0]
+    b = SeqBatch(n, int(n_rows), int(max_new), t.shape[1], max(t.stride(0), t.shape[1]) if n > 1 else t.shape[1],
+                 _int32(row_start, n + 1, "row_start").data_ptr(), _int32(length, n, "length").data_ptr(), t.data_ptr())
+    b.tensors, b.device = (row_start, length, block_tables), _same_device(row_start, length, block_tables)
+    return b
+
+
+def rope(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+         original_len: float = 0, low_turns: float = 0, high_turns: float = 0, mscale: float = 0) -> Rope:
+    """crf_rope_init: the rotary plan of a model (host only)."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise CrfError(1, f"layout {layout!r} or scaling {scaling!r} unknown")
+    lib, out = load(), Rope()
+    sc = RopeScaling(ROPE_SCALINGS.index(scaling), factor, original_len, low_turns, high_turns, mscale)
+    _err(lib, None, lib.crf_rope_init(ctypes.byref(out), ROPE_LAYOUTS.index(layout), int(rotary_dim), theta,
+                                      ctypes.byref(sc)))
+    return out
+
+
+def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePool, layer: int, q_out=None,
+                positions=None, stream=None):
+    """crf_rope_append: q rotated into q_out (both None: keys and values only), k rotated and v into the pages."""
+    d, n = ctx.dims, batch.n_rows
+    _check_pool(ctx, pool, layer + 1)
+    qp, qs = _head_rows(ctx, q, n, d.n_q_heads, "q") if q is not None else (None, 0)
+    op, os_ = _head_rows(ctx, q_out, n, d.n_q_heads, "q_out") if q_out is not None else (None, 0)
+    kp, ks = _head_rows(ctx, k, n, d.n_kv_heads, "k")
+    vp, vs = _head_rows(ctx, v, n, d.n_kv_heads, "v")
+    pp = _int32(positions, n, "positions").data_ptr() if positions is not None else None
+    _check_device(ctx, batch, pool, q, k, v, q_out, positions)
+    st = ctx.lib.crf_rope_append(ctx.handle, rope, batch, pp, qp, qs, kp, ks, vp, vs, op, os_, pool, layer,
+                                 _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def paged_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int, out, lse=None, scale: float = 0.0,
+                    window: int = 0, stream=None):
+    """crf_paged_attention: out [rows, heads, head_dim] (and lse, fp32 [rows, heads]) of the new tokens' queries q."""
+    d, n = ctx.dims, batch.n_rows
+    _check_pool(ctx, pool, layer + 1)
+    qp, qs = _head_rows(ctx, q, n, d.n_q_heads, "q")
+    op, os_ = _head_rows(ctx, out, n, d.n_q_heads, "out")
+    if lse is not None:
+        import torch
+        if lse.dtype is not torch.float32 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
+            raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
+    _check_device(ctx, batch, pool, q, out, lse)
+    st = ctx.lib.crf_paged_attention(ctx.handle, batch, qp, qs, pool, layer, scale, window, op, os_, _ptr(lse),
+                                     _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def pages_copy(ctx: Context, pool: PagePool, src, dst, l0: int = 0, h: Optional[int] = None,
+               to: Optional[PagePool] = None, to_l0: Optional[int] = None, stream=None):
+    """crf_pages_copy: pages src of `pool` to pages dst of `to` (None: the same pool), layers [l0, l0 + h)."""
+    h = pool.tensors[0].shape[0] - l0 if h is None else h
+    to, to_l0 = pool if to is None else to, l0 if to_l0 is None else to_l0
+    _check_pool(ctx, pool, l0 + h)
+    _check_pool(ctx, to, to_l0 + h)
+    n = src.numel()
+    sp, dp = _int32(src, n, "src").data_ptr(), _int32(dst, n, "dst").data_ptr()
+    _check_device(ctx, pool, to, src, dst)
+    st = ctx.lib.crf_pages_copy(ctx.handle, pool, l0, to, to_l0, h, n, sp, dp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def page_map(refs, block_tables, lengths, page_size: int) -> PageMap:
+    """refs [pages], block_tables [S, pages of a sequence], lengths [S]: int32 device tensors."""
+    t = _tables(block_tables)
+    n = t.shape[0]
+    m = PageMap(_int32(refs, None, "refs").data_ptr(), t.data_ptr(), _int32(lengths, n, "lengths").data_ptr(),
+                max(t.stride(0), t.shape[1]) if n > 1 else t.shape[1], refs.numel(), int(page_size), n, t.shape[1])
+    m.tensors, m.device = (refs, block_tables, lengths), _same_device(refs, block_tables, lengths)
+    return m
+
+
+def pages_fork(ctx: Context, pool: PagePool, map: PageMap, parents, children, stream=None):
+    """crf_pages_fork: children[i] becomes a copy of parents[i] that shares its full pages."""
+    _check_pool(ctx, pool, ctx.dims.n_layers)
+    n = parents.numel()
+    pp, cp = _int32(parents, n, "parents").data_ptr(), _int32(children, n, "children").data_ptr()
+    _check_device(ctx, pool, map, parents, children)
+    st = ctx.lib.crf_pages_fork(ctx.handle, pool, map, n, pp, cp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def pages_extend(ctx: Context, map: PageMap, n_new, stream=None):
+    """crf_pages_extend: every sequence s grows by n_new[s] tokens."""
+    gp = _int32(n_new, map.n_seqs, "n_new").data_ptr()
+    _check_device(ctx, map, n_new)
+    st = ctx.lib.crf_pages_extend(ctx.handle, map, gp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def pages_free(ctx: Context, map: PageMap, seqs, stream=None):
+    """crf_pages_free: the sequences end."""
+    n = seqs.numel()
+    sp = _int32(seqs, n, "seqs").data_ptr()
+    _check_device(ctx, map, seqs)
+    st = ctx.lib.crf_pages_free(ctx.handle, map, n, sp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def pages_compact(ctx: Context, pool: PagePool, map: PageMap, map_out: PageMap, remap, counts, stream=None):
+    """crf_pages_compact: the pages in use move to the front of the pool; map_out may be map."""
+    _check_pool(ctx, pool, ctx.dims.n_layers)
+    rp, cp = _int32(remap, map.n_pages, "remap").data_ptr(), _int32(counts, 2, "counts").data_ptr()
+    _check_device(ctx, pool, map, map_out, remap, counts)
+    st = ctx.lib.crf_pages_compact(ctx.handle, pool, map, map_out, rp, cp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)

@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libcrf.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "norm.hip", "f32_path.hip", "lora_down.hip", "gemm_bf16.hip", "gemm_skinny.hip", "gemm_mid.hip",
-           "attn_bf16.hip", "drift.hip"]
+           "attn_bf16.hip", "drift.hip", "paged_api.cpp", "rope_append.hip", "paged_attn.hip", "pages.hip"]
 
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

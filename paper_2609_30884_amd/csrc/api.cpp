@@ -10,78 +10,21 @@
 #include <vector>
 
 #include "../../include/crf.h"
+#include "context.hpp"
 #include "kernels.hpp"
+#include "paged.hpp"
 
 using namespace crf;
 
 namespace {
-
 thread_local std::string g_last_error;
-
-struct Timer {
-  uint32_t mask = 0;            // bit k: launches of class k are bracketed by events
-  std::vector<hipEvent_t> ev;   // pairs (start, stop)
-  std::vector<int> kind;        // per pair
-  size_t used = 0;              // pairs recorded since last read
-};
-
-// Pinned host staging of the drift tables of one call; `ev` marks their copy.
-struct DriftStage {
-  void *host = nullptr;
-  size_t bytes = 0;
-  hipEvent_t ev = nullptr;
-  bool recorded = false;
-};
-
 }  // namespace
 
 // runs of consecutive gate/up tiles on one token tile per workgroup whose fused
 // down-projection adapter sums the context holds room for
 constexpr int DN_RUNS = 4;
 
-struct crf_context {
-  crf_model_dims dims;
-  int32_t max_tokens = 0, max_rank = 0, rank_pad = 0;
-  int device = 0;
-  size_t esz = 2;
-  // workspace
-  float *hres = nullptr;   // [T, d] residual stream, fp32
-  void *xn = nullptr;      // [T, d] normalised input
-  void *q = nullptr;       // [T, dq] rotated queries
-  void *attn = nullptr;    // [T, dq] attention output
-  void *act = nullptr;     // [T, f] SwiGLU output
-  void *u = nullptr;       // bf16: [T, 3*rank_pad] LoRA down-projections; fp32: [T, 3*max_rank] past the fused ranks
-  float2 *rope_cs = nullptr;
-  int *d_err = nullptr;
-  float *attn_part = nullptr;  // bf16 path: key-split attention partials
-  int64_t attn_part_floats = 0;
-  float *lora_part = nullptr;  // bf16 path, <= 16 token rows: parts of the LoRA down-projections
-  int64_t lora_part_floats = 0;
-  // bf16 path: K-part partials of the projections (gemm_part_floats), of which
-  // the 256x256 tiles' last round may fill more (gemm_split_floats)
-  float *gemm_part = nullptr;
-  int64_t gemm_part_floats = 0, gemm_split_floats = 0;
-  float *dn_part = nullptr;    // bf16 path: down-projection adapter sums fused into gate/up
-  int *dn_head = nullptr;      //   and the table of their first tiles
-  unsigned *tickets = nullptr; // bf16 path: arrival counters of K-split workgroups, zero between launches
-  int n_tickets = 0;
-  int n_cu = 0;
-  // drift staging
-  DriftStage drift_stage[4];
-  unsigned drift_next = 0;  // stage of the next call
-  void *drift_dev = nullptr;
-  size_t drift_dev_bytes = 0;
-  std::string last_error;
-  Timer timer;
-  // batched calls over independent caches: a second workspace (a context of
-  // the same shape, made by the first such call) and two lane streams forked
-  // from the caller's stream
-  crf_context *lane2 = nullptr;
-  hipStream_t lane_s[2] = {nullptr, nullptr};
-  hipEvent_t fork_ev = nullptr, join_ev[2] = {nullptr, nullptr};
-};
-
-namespace {
+namespace crf {
 
 crf_status fail(crf_context *ctx, crf_status st, const char *fmt, ...) {
   char buf[512];
@@ -96,13 +39,9 @@ crf_status fail(crf_context *ctx, crf_status st, const char *fmt, ...) {
   return st;
 }
 
-#define HIP_TRY(ctx, expr)                                                                       \
-  do {                                                                                           \
-    hipError_t e_ = (expr);                                                                      \
-    if (e_ != hipSuccess) return fail(ctx, CRF_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+}  // namespace crf
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+namespace {
 
 int dq_of(const crf_model_dims &d) { return d.n_q_heads * d.head_dim; }
 int dkv_of(const crf_model_dims &d) { return d.n_kv_heads * d.head_dim; }
@@ -230,43 +169,6 @@ crf_status check_request(crf_context *ctx, const crf_model_dims *dims, const voi
   }
   return CRF_OK;
 }
-
-// ----------------------------------------------------------------------------- timing
-
-struct Launch {
-  crf_context *ctx;
-  hipStream_t s;
-  int kind;
-  size_t idx = 0;
-  bool on;
-  Launch(crf_context *c, hipStream_t st, int k) : ctx(c), s(st), kind(k), on(((c->timer.mask >> k) & 1u) != 0) {
-    Timer &t = ctx->timer;
-    if (!on) return;
-    idx = t.used;
-    if (2 * idx + 2 > t.ev.size()) {
-      hipEvent_t a, b;
-      if (hipEventCreate(&a) != hipSuccess || hipEventCreate(&b) != hipSuccess) return;
-      t.ev.push_back(a);
-      t.ev.push_back(b);
-      t.kind.push_back(k);
-    }
-    t.kind[idx] = k;
-    (void)hipEventRecord(t.ev[2 * idx], s);
-  }
-  ~Launch() {
-    Timer &t = ctx->timer;
-    if (!on || 2 * idx + 2 > t.ev.size()) return;
-    (void)hipEventRecord(t.ev[2 * idx + 1], s);
-    t.used = idx + 1;
-  }
-};
-
-#define LAUNCH(ctx, s, kind, expr)                                                                     \
-  do {                                                                                                 \
-    Launch lt_(ctx, s, kind);                                                                          \
-    hipError_t e_ = (expr);                                                                            \
-    if (e_ != hipSuccess) return fail(ctx, CRF_ERR_HIP, "launch %s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
 
 // ----------------------------------------------------------------------------- layer sequences
 
@@ -1128,7 +1030,8 @@ void crf_context_destroy(crf_context *ctx) {
   if (!ctx) return;
   void *bufs[] = {ctx->hres, ctx->xn, ctx->q, ctx->attn, ctx->act, ctx->u, ctx->rope_cs,
                   ctx->d_err, ctx->drift_dev, ctx->attn_part, ctx->lora_part, ctx->gemm_part,
-                  ctx->dn_part, ctx->dn_head, ctx->tickets};
+                  ctx->dn_part, ctx->dn_head, ctx->tickets, ctx->paged_ws,
+                  ctx->dims.dtype == CRF_F32 ? ctx->paged_part : nullptr};
   for (void *b : bufs)
     if (b) (void)hipFree(b);
   for (DriftStage &st : ctx->drift_stage) {
@@ -1160,6 +1063,8 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
   ctx->rank_pad = ((max_lora_rank + 15) / 16) * 16;
   ctx->esz = dims->dtype == CRF_BF16 ? 2 : 4;
   (void)hipGetDevice(&ctx->device);
+  if (hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, ctx->device) != hipSuccess)
+    ctx->n_cu = 0;
   const size_t T = (size_t)max_tokens, D = dims->d_model, dq = dq_of(*dims), dkv = dkv_of(*dims), f = dims->d_ffn;
   const size_t e = ctx->esz;
   auto cleanup = [&](crf_status s) {
@@ -1189,8 +1094,6 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
     if ((st = dmalloc(ctx, &ctx->lora_part, (size_t)ctx->lora_part_floats * 4)) != CRF_OK) return cleanup(st);
     // one 256x256 fp32 partial per compute unit, and a second for K-parts in two
     // rounds where a down projection can have more tiles than half the units
-    if (hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, ctx->device) != hipSuccess)
-      ctx->n_cu = 0;
     ctx->gemm_part_floats = (int64_t)std::max(ctx->n_cu, 0) * 256 * 256;
     ctx->gemm_split_floats =
         ctx->gemm_part_floats * (2 * ((T + 255) / 256) * ((D + 255) / 256) > (size_t)std::max(ctx->n_cu, 0) ? 2 : 1);
@@ -1201,6 +1104,8 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
     if (ctx->gemm_part_floats > 0 &&
         (st = dmalloc(ctx, &ctx->gemm_part, (size_t)ctx->gemm_split_floats * 4)) != CRF_OK)
       return cleanup(st);
+    ctx->paged_part = ctx->gemm_part;
+    ctx->paged_part_floats = ctx->gemm_part_floats;
     // fused down-projection adapter sums: DN_RUNS runs of [2][256][16] per
     // compute unit, and one table entry per gate/up tile
     if (ctx->n_cu > 0 && max_lora_rank > 0) {
@@ -1212,7 +1117,12 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
   } else {
     const size_t ur = max_lora_rank > F32_FUSED_RANK ? 3 * (size_t)max_lora_rank : 0;
     if ((st = dmalloc(ctx, &ctx->u, T * ur * 4)) != CRF_OK) return cleanup(st);
+    ctx->paged_part_floats = PAGED_PART_FLOATS;
+    if ((st = dmalloc(ctx, &ctx->paged_part, (size_t)ctx->paged_part_floats * 4)) != CRF_OK) return cleanup(st);
   }
+  if ((st = dmalloc(ctx, &ctx->paged_ws, PAGED_WS_BYTES)) != CRF_OK) return cleanup(st);
+  if (hipMemset(ctx->paged_ws, 0, PAGED_WS_BYTES) != hipSuccess)
+    return cleanup(fail(ctx, CRF_ERR_HIP, "context init: hipMemset"));
   if ((st = dmalloc(ctx, &ctx->rope_cs, T * (dims->head_dim / 2) * sizeof(float2))) != CRF_OK) return cleanup(st);
   if ((st = dmalloc(ctx, &ctx->d_err, sizeof(int))) != CRF_OK) return cleanup(st);
   hipError_t he = hipMemset(ctx->d_err, 0, sizeof(int));

@@ -1,0 +1,437 @@
+// The pages of a cache that many sequences share: copying, forking, extending,
+// freeing and compacting them, with the map (how many sequences hold each page,
+// block tables, lengths) on the device.
+//
+// Every choice is deterministic: free pages are taken lowest first, in the order
+// of the sequences that need them.  A plan is made by one workgroup, which holds
+// one bit per page in LDS (bit set: the page is in use), counts the bits of a
+// run of words per thread and scans the counts; the pages' bytes are moved by a
+// launch of its own over all compute units.  Moving the bytes is HBM bound.
+#include "paged.hpp"
+
+namespace crf {
+namespace {
+
+constexpr int PNT = 1024;               // threads of a plan
+constexpr int PAGE_WORDS = PAGED_MAX_PAGES / 64;  // 64 KB of LDS
+
+// Exclusive prefix sum of v over the workgroup's PNT threads; *total the sum.
+CRF_DEV int block_scan(int v, int *wsum, int *total) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // (wsum of an earlier scan has been read)
+  if (lane == 63) wsum[wave] = x;
+  __syncthreads();
+  int base = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < PNT / 64; ++w) {
+    const int t = wsum[w];
+    if (w < wave) base += t;
+    sum += t;
+  }
+  *total = sum;
+  return base + x - v;
+}
+
+// bits[w]: pages 64 w .. 64 w + 63 in use; pages past n_pages count as `pad`.
+CRF_DEV void load_bits(const int32_t *refs, int n_pages, uint64_t *bits, bool pad) {
+  const int lane = threadIdx.x % 64, words = (n_pages + 63) / 64;
+  for (int w0 = threadIdx.x / 64; w0 < words; w0 += 8 * (PNT / 64)) {
+    int r[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = (w0 + k * (PNT / 64)) * 64 + lane;
+      r[k] = i < n_pages ? refs[i] : (int)pad;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int w = w0 + k * (PNT / 64);
+      const uint64_t m = __builtin_amdgcn_ballot_w64(r[k] > 0);
+      if (lane == 0 && w < words) bits[w] = m;
+    }
+  }
+  __syncthreads();
+}
+
+// ---------------------------------------------------------------- copying
+
+// Chunks of 16 bytes: pair i holds 2 pools x layers x cpp of them.  A thread takes
+// CUN of a pair's chunks, NT apart, all loads in flight before the first store.
+constexpr int CNT = 256, CUN = 8;
+
+struct CopyArgs {
+  PagePools from, to;
+  int per_pair, blocks_per_pair, cpp;  // chunks of a pair; workgroups of a pair; chunks of a page
+  FastDiv cpp_div;
+  int half;                            // layers * cpp: chunks of the K pool
+  int n;
+  const int32_t *n_dev;                // compaction: the number of pairs
+  int *err;
+};
+
+CRF_DEV void copy_pair(const CopyArgs &a, int sp, int dp, int first) {
+  const char *s[CUN];
+  char *d[CUN];
+  u32x4 x[CUN];
+#pragma unroll
+  for (int u = 0; u < CUN; ++u) {
+    int c = first + u * CNT + threadIdx.x;
+    s[u] = nullptr;
+    if (c >= a.per_pair) continue;
+    const bool v = c >= a.half;
+    if (v) c -= a.half;
+    const int l = div_by(c, a.cpp_div), o = c - l * a.cpp;
+    s[u] = (v ? a.from.v : a.from.k) + l * a.from.layer_bytes + sp * a.from.page_bytes + (int64_t)o * 16;
+    d[u] = (v ? a.to.v : a.to.k) + l * a.to.layer_bytes + dp * a.to.page_bytes + (int64_t)o * 16;
+    x[u] = ld16(s[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < CUN; ++u)
+    if (s[u]) st16(d[u], x[u]);
+}
+
+__global__ __launch_bounds__(CNT) void pages_copy_kernel(const CopyArgs a, const int32_t *src, const int32_t *dst) {
+  const int64_t blocks = (int64_t)a.n * a.blocks_per_pair;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const int i = (int)(b / a.blocks_per_pair), part = (int)(b % a.blocks_per_pair);
+    const int sp = src[i], dp = dst[i];
+    if (sp < 0 || sp >= a.from.n_pages || dp < 0 || dp >= a.to.n_pages) {
+      if (threadIdx.x == 0) atomicOr(a.err, (int)CRF_DEVERR_BLOCK_TABLE);
+      continue;
+    }
+    copy_pair(a, sp, dp, part * CNT * CUN);
+  }
+}
+
+CopyArgs copy_args(const PagePools &from, const PagePools &to, int layers, int bytes, int n, int *err) {
+  CopyArgs a{};
+  a.from = from;
+  a.to = to;
+  a.cpp = bytes / 16;
+  a.half = layers * a.cpp;
+  a.per_pair = 2 * a.half;
+  a.blocks_per_pair = (a.per_pair + CNT * CUN - 1) / (CNT * CUN);
+  a.cpp_div = fast_div(a.cpp);
+  a.n = n;
+  a.err = err;
+  return a;
+}
+
+// ---------------------------------------------------------------- forking
+
+// state[i]: the page that takes the copy of fork i's begun page, -1 where it needs
+// none, -2 where the fork is refused.  A child that is named twice is forked by the
+// first that names it.
+__global__ __launch_bounds__(PNT) void fork_plan_kernel(const PageMap m, int n, const int32_t *parents,
+                                                        const int32_t *children, int32_t *state) {
+  __shared__ uint64_t bits[PAGE_WORDS];
+  __shared__ int plen[PAGED_MAX_LIST], need[PAGED_MAX_LIST], claim[PAGED_MAX_LIST];
+  __shared__ int wsum[PNT / 64];
+  const int tid = threadIdx.x;
+  for (int s = tid; s < m.n_seqs; s += PNT) claim[s] = n;
+  load_bits(m.refs, m.n_pages, bits, true);
+  for (int i = tid; i < n; i += PNT) {
+    const int p = parents[i], c = children[i];
+    plen[i] = -1;
+    if (p < 0 || p >= m.n_seqs || c < 0 || c >= m.n_seqs || p == c || m.lengths[c] != 0) continue;
+    const int len = m.lengths[p];
+    if (len < 0 || (int64_t)len > (int64_t)m.max_pages * m.page_size) continue;
+    plen[i] = len;
+    atomicMin(&claim[c], i);
+  }
+  __syncthreads();
+  int wanted = 0;  // forks that need a page
+  for (int i0 = 0; i0 < n; i0 += PNT) {
+    const int i = i0 + tid;
+    bool want = false;
+    if (i < n) {
+      if (plen[i] >= 0 && claim[children[i]] != i) plen[i] = -1;
+      want = plen[i] > 0 && plen[i] % m.page_size != 0;
+      state[i] = plen[i] < 0 ? -2 : -1;
+      if (plen[i] < 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+    }
+    int total;
+    const int at = wanted + block_scan(want, wsum, &total);
+    if (want) need[at] = i;
+    wanted += total;
+  }
+  __syncthreads();
+  // free pages in ascending order, one to each
+  const int words = (m.n_pages + 63) / 64, per = (words + PNT - 1) / PNT;
+  const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
+  int free = 0, n_free;
+  for (int w = w0; w < w1; ++w) free += __popcll(~bits[w]);
+  int rank = block_scan(free, wsum, &n_free);
+  for (int w = w0; w < w1 && rank < wanted; ++w)
+    for (uint64_t f = ~bits[w]; f && rank < wanted; f &= f - 1, ++rank) {
+      const int page = 64 * w + __builtin_ctzll(f);
+      state[need[rank]] = page;
+      m.refs[page] = 1;
+    }
+  for (int k = n_free + tid; k < wanted; k += PNT) {
+    state[need[k]] = -2;
+    plen[need[k]] = -1;
+    atomicOr(m.err, (int)CRF_DEVERR_PAGES);
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += PNT)
+    if (plen[i] >= 0) m.lengths[children[i]] = plen[i];
+}
+
+// Block row 0 of a fork: its table row and the counts of the full pages that it
+// shares; the others copy the begun page.
+__global__ __launch_bounds__(CNT) void fork_apply_kernel(const PageMap m, const CopyArgs a, const int32_t *parents,
+                                                         const int32_t *children, const int32_t *state) {
+  const int i = blockIdx.y, page = state[i];
+  if (page == -2) return;
+  const int32_t *from = m.tables + (int64_t)parents[i] * m.table_stride;
+  int32_t *to = m.tables + (int64_t)children[i] * m.table_stride;
+  const int len = m.lengths[children[i]], full = len / m.page_size;
+  if (blockIdx.x == 0) {
+    for (int j = threadIdx.x; j < full; j += CNT) {
+      const int e = from[j];
+      to[j] = e;
+      if (e < 0 || e >= m.n_pages)
+        atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
+      else
+        atomicAdd(&m.refs[e], 1);
+    }
+    if (threadIdx.x == 0 && page >= 0) to[full] = page;
+    return;
+  }
+  if (page < 0) return;
+  const int sp = from[full];
+  if (sp < 0 || sp >= m.n_pages) {
+    if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
+    return;
+  }
+  copy_pair(a, sp, page, (blockIdx.x - 1) * CNT * CUN);
+}
+
+// ---------------------------------------------------------------- extending
+
+// Every sequence s grows by n_new[s] tokens; the pages that this takes are the
+// lowest free ones, in the order of the sequences.  The first sequence for which
+// too few are left and every later one that needs any keep their length.
+__global__ __launch_bounds__(PNT) void extend_kernel(const PageMap m, const int32_t *n_new) {
+  __shared__ uint64_t bits[PAGE_WORDS];
+  __shared__ int first[PAGED_MAX_LIST + 1];  // pages wanted before a sequence's
+  __shared__ int wsum[PNT / 64];
+  const int tid = threadIdx.x;
+  auto grow = [&](int s, int &len, int &held) {  // tokens that sequence s asks for, -1 when it may not
+    const int g = n_new[s];
+    len = m.lengths[s];
+    held = 0;
+    if (g == 0) return 0;
+    if (g < 0 || len < 0 || (int64_t)len + g > (int64_t)m.max_pages * m.page_size) return -1;
+    held = (len + m.page_size - 1) / m.page_size;
+    return g;
+  };
+  load_bits(m.refs, m.n_pages, bits, true);
+  int wanted = 0;
+  for (int s0 = 0; s0 < m.n_seqs; s0 += PNT) {
+    const int s = s0 + tid;
+    int need = 0, total;
+    if (s < m.n_seqs) {
+      int len, held;
+      const int g = grow(s, len, held);
+      if (g > 0) need = (len + g + m.page_size - 1) / m.page_size - held;
+      if (g < 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+    }
+    const int at = wanted + block_scan(need, wsum, &total);
+    if (s < m.n_seqs) first[s] = min(at, 1 << 30);  // (a table has at most 2^19 entries)
+    wanted = min(wanted + total, 1 << 30);
+  }
+  if (tid == 0) first[m.n_seqs] = wanted;
+  const int words = (m.n_pages + 63) / 64, per = (words + PNT - 1) / PNT;
+  const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
+  int free = 0, n_free;
+  for (int w = w0; w < w1; ++w) free += __popcll(~bits[w]);
+  int rank = block_scan(free, wsum, &n_free);
+  for (int w = w0; w < w1 && rank < wanted; ++w)
+    for (uint64_t f = ~bits[w]; f && rank < wanted; f &= f - 1, ++rank) {
+      int lo = 0, hi = m.n_seqs;  // the last sequence whose first page is at most the rank-th
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first[mid] <= rank) lo = mid;
+        else hi = mid;
+      }
+      if (first[lo + 1] > n_free) continue;
+      const int page = 64 * w + __builtin_ctzll(f);
+      int len, held;
+      (void)grow(lo, len, held);
+      m.tables[(int64_t)lo * m.table_stride + held + rank - first[lo]] = page;
+      m.refs[page] = 1;
+    }
+  __syncthreads();
+  for (int s = tid; s < m.n_seqs; s += PNT) {
+    int len, held;
+    const int g = grow(s, len, held);
+    if (g <= 0) continue;
+    if (first[s + 1] > first[s] && first[s + 1] > n_free)
+      atomicOr(m.err, (int)CRF_DEVERR_PAGES);
+    else
+      m.lengths[s] = len + g;
+  }
+}
+
+// ---------------------------------------------------------------- freeing
+
+__global__ __launch_bounds__(CNT) void free_kernel(const PageMap m, const int32_t *seqs) {
+  __shared__ int len_s;
+  const int s = seqs[blockIdx.x];
+  if (s < 0 || s >= m.n_seqs) {
+    if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+    return;
+  }
+  // (a sequence that is named twice is freed by whoever takes its length)
+  if (threadIdx.x == 0) len_s = atomicExch(&m.lengths[s], 0);
+  __syncthreads();
+  const int len = len_s;
+  if (len < 0 || (int64_t)len > (int64_t)m.max_pages * m.page_size) {
+    if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+    return;
+  }
+  const int held = (int)(((int64_t)len + m.page_size - 1) / m.page_size);
+  for (int j = threadIdx.x; j < held; j += CNT) {
+    const int e = m.tables[(int64_t)s * m.table_stride + j];
+    if (e < 0 || e >= m.n_pages) {
+      atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
+    } else if (atomicSub(&m.refs[e], 1) <= 0) {  // held by nobody
+      atomicAdd(&m.refs[e], 1);
+      atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- compacting
+
+// With L pages in use, the k-th page in use at or past L moves to the k-th free
+// page below L: no page is both a source and a destination, so the copies need no
+// order and the old map stays readable until its pages are reused.
+__global__ __launch_bounds__(PNT) void compact_plan_kernel(const PageMap m, int32_t *refs_out, int32_t *remap,
+                                                           int32_t *moves, int32_t *counts) {
+  __shared__ uint64_t bits[PAGE_WORDS];
+  __shared__ int wsum[PNT / 64];
+  const int tid = threadIdx.x;
+  load_bits(m.refs, m.n_pages, bits, false);
+  const int words = (m.n_pages + 63) / 64, per = (words + PNT - 1) / PNT;
+  const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
+  int count = 0, live, n_holes, n_moves;
+  for (int w = w0; w < w1; ++w) count += __popcll(bits[w]);
+  (void)block_scan(count, wsum, &live);
+  // word w's pages below L
+  auto below = [&](int w) {
+    return 64 * w + 64 <= live ? ~(uint64_t)0 : 64 * w >= live ? 0 : ((uint64_t)1 << (live - 64 * w)) - 1;
+  };
+  int holes = 0, movers = 0;
+  for (int w = w0; w < w1; ++w) {
+    holes += __popcll(~bits[w] & below(w));
+    movers += __popcll(bits[w] & ~below(w));
+  }
+  int hole = block_scan(holes, wsum, &n_holes), mover = block_scan(movers, wsum, &n_moves);
+  for (int w = w0; w < w1; ++w) {
+    for (uint64_t f = ~bits[w] & below(w); f; f &= f - 1) moves[2 * hole++ + 1] = 64 * w + __builtin_ctzll(f);
+    for (uint64_t f = bits[w] & ~below(w); f; f &= f - 1) moves[2 * mover++] = 64 * w + __builtin_ctzll(f);
+  }
+  if (tid == 0) {
+    counts[0] = live;
+    counts[1] = n_moves;
+  }
+  __syncthreads();
+  for (int k = tid; k < n_moves; k += PNT) {
+    const int src = moves[2 * k], dst = moves[2 * k + 1];
+    remap[src] = dst;
+    refs_out[dst] = m.refs[src];
+  }
+  __syncthreads();
+  for (int p = tid; p < m.n_pages; p += PNT) {
+    const bool used = (bits[p / 64] >> (p % 64)) & 1;
+    if (p < live) {
+      remap[p] = used ? p : -1;
+      if (used) refs_out[p] = m.refs[p];
+    } else {
+      if (!used) remap[p] = -1;
+      refs_out[p] = 0;
+    }
+  }
+}
+
+// The first n_seqs workgroups rewrite a sequence's table each, the others copy.
+__global__ __launch_bounds__(CNT) void compact_apply_kernel(const PageMap m, const PageMap out, const CopyArgs a,
+                                                            const int32_t *remap, const int32_t *moves) {
+  if ((int)blockIdx.x < m.n_seqs) {
+    const int s = blockIdx.x, len = m.lengths[s];
+    if (len < 0 || (int64_t)len > (int64_t)m.max_pages * m.page_size) {
+      if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+      return;
+    }
+    const int held = (int)(((int64_t)len + m.page_size - 1) / m.page_size);
+    for (int j = threadIdx.x; j < held; j += CNT) {
+      const int e = m.tables[(int64_t)s * m.table_stride + j];
+      const int to = e >= 0 && e < m.n_pages ? remap[e] : -1;
+      if (to < 0) atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
+      out.tables[(int64_t)s * out.table_stride + j] = to;
+    }
+    if (threadIdx.x == 0 && out.lengths != m.lengths) out.lengths[s] = len;
+    return;
+  }
+  const int64_t blocks = (int64_t)*a.n_dev * a.blocks_per_pair;
+  for (int64_t b = blockIdx.x - m.n_seqs; b < blocks; b += gridDim.x - m.n_seqs) {
+    const int i = (int)(b / a.blocks_per_pair), part = (int)(b % a.blocks_per_pair);
+    copy_pair(a, moves[2 * i], moves[2 * i + 1], part * CNT * CUN);
+  }
+}
+
+// workgroups of a copy whose count only the device knows: eight to a CU
+constexpr int COPY_GRID = 2048;
+
+}  // namespace
+
+hipError_t launch_pages_copy(hipStream_t s, const PagePools &from, const PagePools &to, int layers, int bytes, int n,
+                             const int32_t *src, const int32_t *dst, int *err) {
+  if (n <= 0 || layers <= 0) return hipSuccess;
+  CopyArgs a = copy_args(from, to, layers, bytes, n, err);
+  const int64_t blocks = (int64_t)n * a.blocks_per_pair;
+  hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(CNT), 0, s, a,
+                     src, dst);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(hipStream_t s, const PageMap &m, const PagePools &pool, int layers, int bytes, int n,
+                             const int32_t *parents, const int32_t *children, int32_t *state) {
+  if (n <= 0) return hipSuccess;
+  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(PNT), 0, s, m, n, parents, children, state);
+  const CopyArgs a = copy_args(pool, pool, layers, bytes, n, m.err);
+  hipLaunchKernelGGL(fork_apply_kernel, dim3(1 + a.blocks_per_pair, n), dim3(CNT), 0, s, m, a, parents, children,
+                     state);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_extend(hipStream_t s, const PageMap &m, const int32_t *n_new) {
+  if (m.n_seqs <= 0) return hipSuccess;
+  hipLaunchKernelGGL(extend_kernel, dim3(1), dim3(PNT), 0, s, m, n_new);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_free(hipStream_t s, const PageMap &m, int n, const int32_t *seqs) {
+  if (n <= 0) return hipSuccess;
+  hipLaunchKernelGGL(free_kernel, dim3(n), dim3(CNT), 0, s, m, seqs);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(hipStream_t s, const PageMap &in, const PageMap &out, const PagePools &pool, int layers,
+                                int bytes, int32_t *remap, int32_t *moves, int32_t *counts) {
+  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(PNT), 0, s, in, out.refs, remap, moves, counts);
+  CopyArgs a = copy_args(pool, pool, layers, bytes, in.n_pages / 2, in.err);
+  a.n_dev = counts + 1;
+  hipLaunchKernelGGL(compact_apply_kernel, dim3(in.n_seqs + COPY_GRID), dim3(CNT), 0, s, in, out, a, remap, moves);
+  return hipGetLastError();
+}
+
+}  // namespace crf

@@ -1,0 +1,262 @@
+"""Copying, forking, extending, freeing and compacting pages against a model of
+the map in Python; the bytes of pages exactly."""
+import random
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Server:
+    """A pool, its map on the device, and the same map as Python lists."""
+
+    def __init__(self, n_pages, n_seqs, width, page=16, nkv=2, hd=64, layers=3, dtype=torch.bfloat16, seed=0):
+        import paper_2609_30884_amd as crf
+        from tests.paged import context
+        self.crf, self.page = crf, page
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.ctx = context(2 * nkv, nkv, hd, dtype, layers=layers)
+        self.k, self.v = (torch.randn(layers, n_pages, nkv, page, hd, generator=g, device="cuda").to(dtype)
+                          for _ in range(2))
+        self.pool = crf.page_pool(self.k, self.v, page)
+        self.refs, self.tables, self.lengths = [0] * n_pages, [[-7] * width for _ in range(n_seqs)], [0] * n_seqs
+        self.width = width
+        self.upload()
+
+    def upload(self):
+        self.d = [_i32(self.refs), _i32(self.tables).reshape(len(self.tables), self.width), _i32(self.lengths)]
+        self.map = self.crf.page_map(*self.d, self.page)
+
+    def up(self, n):
+        return -(-n // self.page)
+
+    def check(self, flags=0):
+        torch.cuda.synchronize()
+        assert self.ctx.device_errors() == flags
+        assert self.d[0].tolist() == self.refs
+        assert self.d[2].tolist() == self.lengths
+        assert self.d[1].tolist() == self.tables
+
+    # the model
+    def free_pages(self):
+        return [p for p, c in enumerate(self.refs) if c <= 0]
+
+    def extend(self, grow):
+        free, flags, out = self.free_pages(), 0, False
+        wanted = 0
+        for s, g in enumerate(grow):
+            if g == 0:
+                continue
+            if g < 0 or self.lengths[s] + g > self.width * self.page:
+                flags |= 2
+                continue
+            held, need = self.up(self.lengths[s]), self.up(self.lengths[s] + g) - self.up(self.lengths[s])
+            wanted += need
+            if need and wanted > len(free):
+                flags |= 4
+                continue
+            for j in range(need):
+                p = free[wanted - need + j]
+                self.tables[s][held + j] = p
+                self.refs[p] = 1
+            self.lengths[s] += g
+        self.crf.pages_extend(self.ctx, self.map, _i32(grow))
+        self.check(flags)
+
+    def fork(self, parents, children):
+        k, v = self.k.clone(), self.v.clone()
+        free, flags = self.free_pages(), 0
+        before, taken = list(self.lengths), set()
+        for a, b in zip(parents, children):
+            n = len(before)
+            if not (0 <= a < n and 0 <= b < n) or a == b or before[b] != 0 or b in taken:
+                flags |= 2
+                continue
+            taken.add(b)
+            full, tail = before[a] // self.page, before[a] % self.page
+            if tail:
+                if not free:
+                    flags |= 4
+                    continue
+                p = free.pop(0)
+                self.refs[p] = 1
+                src = self.tables[a][full]
+                k[:, p], v[:, p] = k[:, src], v[:, src]
+            for j in range(full):
+                self.tables[b][j] = self.tables[a][j]
+                self.refs[self.tables[a][j]] += 1
+            if tail:
+                self.tables[b][full] = p
+            self.lengths[b] = before[a]
+        self.crf.pages_fork(self.ctx, self.pool, self.map, _i32(parents), _i32(children))
+        self.check(flags)
+        assert torch.equal(self.k, k) and torch.equal(self.v, v)
+
+    def free(self, seqs):
+        flags = 0
+        for s in seqs:
+            if not 0 <= s < len(self.lengths):
+                flags |= 2
+                continue
+            for j in range(self.up(self.lengths[s])):
+                self.refs[self.tables[s][j]] -= 1
+            self.lengths[s] = 0
+        self.crf.pages_free(self.ctx, self.map, _i32(seqs))
+        self.check(flags)
+
+    def compact(self, in_place=True):
+        k, v = self.k.clone(), self.v.clone()
+        old = [t.clone() for t in self.d]
+        live = [p for p, c in enumerate(self.refs) if c > 0]
+        n = len(live)
+        moved, holes = [p for p in live if p >= n], [p for p in range(n) if self.refs[p] <= 0]
+        to = {p: p for p in live}
+        to.update(zip(moved, holes))
+        refs = [0] * len(self.refs)
+        for p in range(n):
+            refs[p] = self.refs[p]
+        for a, b in zip(moved, holes):
+            k[:, b], v[:, b] = k[:, a], v[:, a]
+            refs[b] = self.refs[a]
+        if in_place:
+            out, out_map = self.d, self.map
+        else:
+            out = [torch.full_like(t, -7) for t in self.d]
+            out_map = self.crf.page_map(*out, self.page)
+            self.tables = [[-7] * self.width for _ in self.tables]
+        tables = old[1].tolist()
+        for s, length in enumerate(self.lengths):
+            for j in range(self.up(length)):
+                self.tables[s][j] = to[tables[s][j]]
+        self.refs = refs
+        remap, counts = torch.zeros_like(self.d[0]), _i32([0, 0])
+        self.crf.pages_compact(self.ctx, self.pool, self.map, out_map, remap, counts)
+        torch.cuda.synchronize()
+        if not in_place:
+            assert all(torch.equal(a, b) for a, b in zip(old, self.d))  # the old map is as it was
+        self.d, self.map = out, out_map
+        self.check()
+        assert counts.tolist() == [n, len(moved)]
+        assert remap.tolist() == [to.get(p, -1) for p in range(len(refs))]
+        assert torch.equal(self.k, k) and torch.equal(self.v, v)
+
+
+@pytest.mark.parametrize("page,nkv,hd,layers,dtype", [(16, 2, 64, 3, "bfloat16"), (1, 2, 64, 1, "bfloat16"),
+                                                      (8, 1, 64, 2, "float32"), (32, 4, 128, 2, "bfloat16"),
+                                                      (7, 3, 128, 5, "float32")])
+def test_copies(page, nkv, hd, layers, dtype):
+    print(f"[case] copies page {page} {nkv} x {hd} {dtype}", flush=True)
+    s = Server(90, 1, 4, page, nkv, hd, layers, getattr(torch, dtype))
+    for n in (1, 2, 45):
+        order = torch.randperm(90, generator=torch.Generator().manual_seed(n))
+        src, dst = order[:n], order[n:2 * n]
+        for l0, h in ((0, layers), (layers - 1, 1), (0, 0)):
+            k, v = s.k.clone(), s.v.clone()
+            k[l0:l0 + h, dst], v[l0:l0 + h, dst] = k[l0:l0 + h, src], v[l0:l0 + h, src]
+            s.crf.pages_copy(s.ctx, s.pool, src.int().cuda(), dst.int().cuda(), l0, h)
+            torch.cuda.synchronize()
+            assert torch.equal(s.k, k) and torch.equal(s.v, v)
+    # into a padded pool of one layer, one page twice, and pages out of range
+    big = torch.zeros(1, 7, nkv * page * hd + 8, dtype=s.k.dtype, device="cuda")
+    to = [b[..., :-8].unflatten(-1, (nkv, page, hd)) for b in (big, big.clone())]
+    src, dst = _i32([89, 3, 3, -1, 90, 4]), _i32([6, 0, 1, 2, 3, 7])
+    s.crf.pages_copy(s.ctx, s.pool, src, dst, layers - 1, 1, s.crf.page_pool(*to, page), 0)
+    torch.cuda.synchronize()
+    assert s.ctx.device_errors() == 1
+    for a, b in zip((s.k, s.v), to):
+        assert torch.equal(b[0, [6, 0, 1]], a[layers - 1, [89, 3, 3]])
+        assert (b[0, 2:6] == 0).all()
+    assert (big[..., -8:] == 0).all()
+
+
+def test_extend():
+    print("[case] extend", flush=True)
+    s = Server(40, 6, 9)
+    s.extend([1, 0, 16, 17, 0, 33])
+    s.extend([15, 5, 1, 0, 0, 0])
+    s.extend([1, -1, 0, 145, 2, 0])       # a negative one, one past its table
+    s.extend([0, 0, 0, 100, 140, 144 - 33])  # fits for some
+    s.extend([0] * 6)
+    s.extend([1] * 6)                      # too few pages for the last ones
+    s.free([4, 4, 1, 9, -1])
+    s.extend([200, 30, 0, 0, 20, 0])
+
+
+def test_fork_and_free():
+    print("[case] fork", flush=True)
+    s = Server(60, 12, 9)
+    s.extend([1, 16, 40, 144] + [0] * 8)
+    s.fork([2, 1, 2], [4, 5, 6])
+    s.fork([4, 0, 7], [7, 8, 9])            # of a fork, of one token, of an empty one
+    s.fork([2, 2, 40, -1, 2, 2, 3], [10, 10, 1, 2, 12, 2, 3])  # a child twice, out of range, not empty, itself
+    s.extend([3, 3, 3, 0, 3, 3, 3, 3, 3, 0, 0, 0])
+    s.free([2, 4])
+    s.fork([10, 6], [2, 4])
+    s.free(list(range(12)))
+    assert s.refs == [0] * 60
+    # pages run out in the middle of a call
+    s = Server(9, 6, 4)
+    s.extend([20, 33, 16, 0, 0, 0])
+    s.fork([0, 2, 0], [3, 4, 5])
+    s = Server(8, 6, 4)
+    s.extend([20, 33, 16, 0, 0, 0])
+    s.fork([0, 2, 0], [3, 4, 5])
+
+
+@pytest.mark.parametrize("n_pages,in_place", [(64, True), (65, False), (63, True), (1000, False), (130000, True)])
+def test_compact(n_pages, in_place):
+    print(f"[case] compact {n_pages}", flush=True)
+    rng = random.Random(n_pages)
+    width = 40 if n_pages < 2000 else 3000
+    s = Server(n_pages, 20, width, page=1 if n_pages > 2000 else 16, hd=64, layers=1 if n_pages > 2000 else 3)
+    s.compact(in_place)                       # nothing held
+    order = list(range(n_pages))
+    rng.shuffle(order)
+    for q in range(20):
+        held = rng.randrange(0, min(width, n_pages // 25) + 1)
+        for j in range(held):
+            p = order.pop()
+            s.tables[q][j] = p
+            s.refs[p] = rng.choice([1, 1, 2])
+        s.lengths[q] = max(0, held * s.page - rng.randrange(s.page))
+    s.upload()
+    s.compact(in_place)
+    s.compact(not in_place)                   # nothing to move
+    s.free([1, 3, 5, 7])
+    s.compact(in_place)
+
+
+def test_random_life():
+    """Sequences come, grow, fork, leave; the map equals the model's after every call."""
+    print("[case] life", flush=True)
+    rng = random.Random(5)
+    s = Server(120, 16, 12, page=8, nkv=2, hd=64, layers=2)
+    for _ in range(60):
+        what = rng.choice(["extend", "extend", "fork", "free", "compact"])
+        if what == "extend":
+            s.extend([rng.choice([0, 0, 1, 1, 7, 30]) for _ in range(16)])
+        elif what == "fork":
+            n = rng.randrange(1, 5)
+            s.fork([rng.randrange(16) for _ in range(n)], [rng.randrange(16) for _ in range(n)])
+        elif what == "free":
+            s.free([rng.randrange(16) for _ in range(rng.randrange(1, 6))])
+        else:
+            s.compact(rng.random() < 0.5)
+
+
+def test_map_limits():
+    """4096 sequences and forks, and 2^19 pages."""
+    print("[case] limits", flush=True)
+    s = Server(1 << 19, 4096, 2, page=1, nkv=2, hd=64, layers=1)
+    s.extend([2 if i % 2 else 0 for i in range(4096)])
+    s.fork([2 * i + 1 for i in range(2048)], [2 * i for i in range(2048)])
+    s.refs[(1 << 19) - 1] = 1
+    s.tables[5][0], s.refs[s.tables[5][0]] = (1 << 19) - 1, s.refs[s.tables[5][0]] - 1
+    s.upload()
+    s.compact()
+    s.free(list(range(4096)))
