@@ -45,7 +45,6 @@ constexpr float PSUM_MAX = 256.0f;  // a lane's sum of a block's probabilities t
 constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
 constexpr int ML_CAP = 2048;        // (reference, sum) pairs that a join holds in LDS
 constexpr int MANY = 4;             // units per resident workgroup from which none is split
-constexpr int MIN_KEYS = 256;       // keys that a workgroup is worth
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -69,16 +68,31 @@ struct Layout {
   static constexpr int EPC = 16 / (int)sizeof(T);   // elements of a chunk
   static constexpr int KS = HD / (2 * EPC);         // steps of two chunks along a row
   static constexpr int HB = HD / 32;                // 32-row blocks of O^T
-  // chunk slot of chunk c in K row r: conflict-free 16-byte reads of 8 rows
+  // Chunk c of K row r lies at slot c ^ (r & 15) (8 chunks: r & 7): 16-byte reads of 8
+  // rows land on distinct banks.
   static CRF_DEV int kslot(int r, int c) { return c ^ (r & (CH < 16 ? CH - 1 : 15)); }
-  // and in V row r: bf16 transpose reads of 4 rows land on distinct banks; fp32
-  // rows are read along the row
+  // And of V row r: bf16 transpose reads of 4 rows land on distinct banks; fp32 rows
+  // are read along the row.
   static CRF_DEV int vslot(int r, int c) {
     if (sizeof(T) == 4) return c;
     if (HD == 128) return c ^ ((0xCA60 >> (4 * (r & 3))) & 15);
     return c ^ (2 * (r & 3));
   }
+  // Byte addresses of a lane's reads in a tile, of which the others follow by an XOR
+  // of the chunk bits and by constants: K row l32, chunk g (chunk 2 i + g: ^ 32 i) ...
+  static CRF_DEV uint32_t kaddr(int lane) { return (lane % 32) * ROWB + kslot(lane % 32, lane / 32) * 16; }
+  // ... V by transpose reads: 16-lane group t covers hd 16 (t & 1) .. + 15 of a 32-row
+  // block b of O^T (^ 64 b) and key rows 4 (t / 2) + 0..3; fp32: row 4 g, column l32.
+  static CRF_DEV uint32_t vaddr(int lane) {
+    if (sizeof(T) == 4) return 4 * (lane / 32) * ROWB + lane % 32 * 4;
+    const int t = lane / 16, r = 4 * (t >> 1) + lane % 16 / 4, hd = 16 * (t & 1) + 4 * (lane % 4);
+    return r * ROWB + vslot(r, hd / 8) * 16 + hd % 8 * 2;
+  }
 };
+
+// Keeps a value from being formed once and held through a loop: the few operations
+// that derive addresses from it cost less than the registers.
+CRF_DEV void fresh(uint32_t &x) { asm volatile("" : "+v"(x)); }
 
 // A lane's query row: KS x 16 bytes.
 template <typename T, int HD>
@@ -89,28 +103,6 @@ struct QFrag {
     for (int s = 0; s < Layout<T, HD>::KS; ++s) f[s] = ld16(row + (2 * s + g) * Layout<T, HD>::EPC);
   }
 };
-
-// Raw scores of 32 keys (LDS rows r0 ..) against the wave's 32 rows.
-template <typename T, int HD>
-CRF_DEV f32x16 scores(const T *kt, int r0, const QFrag<T, HD> &q, int g, int l32) {
-  using L = Layout<T, HD>;
-  f32x16 acc;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-  const int r = r0 + l32;
-#pragma unroll
-  for (int s = 0; s < L::KS; ++s) {
-    const u32x4 k = ld16(kt + r * HD + L::kslot(r, 2 * s + g) * L::EPC);
-    if constexpr (sizeof(T) == 2) {
-      acc = mfma32(as_bf16x8(k), as_bf16x8(q.f[s]), acc);
-    } else {
-      const f32x4 a = __builtin_bit_cast(f32x4, k), b = __builtin_bit_cast(f32x4, q.f[s]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc = mfma32f(a[e], b[e], acc);
-    }
-  }
-  return acc;
-}
 
 // The keys that a lane's row sees: [lo, hi]; bad: some pages of the unit are out of
 // range, whose keys nobody sees.
@@ -138,137 +130,185 @@ struct RowState {
 
 CRF_DEV bool not_finite16(int h) { return (h & 0x7f80) == 0x7f80; }
 
-// One block of 32 keys, key0 .. key0 + 31 in LDS rows r0 ..: scores, probabilities,
-// O += P V.  MASK: some row does not see some key of it.  A value that is not finite
-// takes no part in a row that does not see its key, though the product multiplies it
-// by zero: where a masked block holds such values, they are taken out of the product
-// and brought back where a weight is not zero.
-template <typename T, int HD, bool MASK>
-CRF_DEV void block32(const T *kt, const T *vt, int r0, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
-                     int lane, const Seen &seen) {
+// Raw scores of NB blocks of 32 keys (LDS rows r0 ..) against the wave's 32 rows.
+// bf16: the K fragments are read two steps ahead of the products that use them (the
+// scheduling barriers keep the compiler from regrouping them).
+template <typename T, int HD, int NB>
+CRF_DEV void scores(const T *kt, int r0, const QFrag<T, HD> &q, int lane, f32x16 (&s)[NB]) {
   using L = Layout<T, HD>;
-  const int g = lane / 32, l32 = lane % 32;
-  f32x16 s = scores<T, HD>(kt, r0, q, g, l32);
-  if constexpr (MASK) {
+  f32x16 zero;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int key = key0 + 8 * (v / 4) + 4 * g + v % 4;
-      bool hide = key < seen.lo || key > seen.hi;
-      if (seen.bad && !hide) hide = seen.pages[div_by(key, seen.ps_div) - seen.first] < 0;
-      if (hide) s[v] = -INFINITY;
+  for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+  u32x4 kf[3][NB];
+  uint32_t ka = L::kaddr(lane);
+  fresh(ka);
+  auto kread = [&](int step, u32x4 (&f)[NB]) {
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) f[kb] = ld16((const char *)kt + (r0 + 32 * kb) * L::ROWB + (ka ^ (32 * step)));
+  };
+  kread(0, kf[0]);
+  kread(1, kf[1]);
+#pragma unroll
+  for (int i = 0; i < L::KS; ++i) {
+    if (i + 2 < L::KS) kread(i + 2, kf[(i + 2) % 3]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      if constexpr (sizeof(T) == 2) {
+        s[kb] = mfma32(as_bf16x8(kf[i % 3][kb]), as_bf16x8(q.f[i]), i == 0 ? zero : s[kb]);
+      } else {
+        const f32x4 a = __builtin_bit_cast(f32x4, kf[i % 3][kb]), b = __builtin_bit_cast(f32x4, q.f[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[kb] = mfma32f(a[e], b[e], i == 0 && e == 0 ? zero : s[kb]);
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  float p[16], sum = 0.f;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    p[v] = fast_exp2(fmaf(s[v], c, -st.ref));
-    sum += p[v];
-  }
-  if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {  // (also where the sum is no number)
-    float mx = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
-    // only rows that need one: a row's result does not depend on the tile's others
-    const float other = __shfl_xor(sum, 32, 64);
-    const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
-    const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
-    const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
-    const float base = ref == -INFINITY ? 0.f : ref;
-    st.ref = ref;
-    st.l *= alpha;
-#pragma unroll
-    for (int b = 0; b < L::HB; ++b) st.o[b] *= alpha;
-    sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      p[v] = fast_exp2(fmaf(s[v], c, -base));
-      sum += p[v];
-    }
-  }
-  st.l += sum;
+}
 
+// O += P V for the probabilities p of 32 keys in LDS rows r0 ...  MASK: a value that
+// is not finite takes no part in a row that does not see its key (p = 0), though the
+// product multiplies it by zero: such values are taken out of the product and added
+// where the weight is not zero.
+template <typename T, int HD, bool MASK>
+CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, int lane) {
+  using L = Layout<T, HD>;
+  uint32_t va = L::vaddr(lane);
+  fresh(va);
   if constexpr (sizeof(T) == 2) {
     bf16x8 pf[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 8; ++e) pf[h][e] = f2bf(p[8 * h + e]);
-    // transpose reads: 16-lane group t covers hd 16 (t & 1) .. + 15 of a 32-row block
-    // and key rows 4 (t / 2) + 0..3; slots 4-7 hold the rows 8 further on
-    const int tg = lane / 16;
-    const int tk = 4 * (tg >> 1) + (lane % 16) / 4, th = 16 * (tg & 1) + 4 * (lane % 4);
+    // slots 4-7 of a fragment hold the rows 8 further on
 #pragma unroll
     for (int b = 0; b < L::HB; ++b) {
-      const int hd = 32 * b + th;
+      s16x4 x[2][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int ra = r0 + 16 * h + tk, rb = ra + 8;
-        const s16x4 lo = ld_tr(vt + ra * HD + L::vslot(ra, hd / 8) * 8 + hd % 8);
-        const s16x4 hi = ld_tr(vt + rb * HD + L::vslot(rb, hd / 8) * 8 + hd % 8);
-        s16x4 x[2] = {lo, hi};
-        if constexpr (MASK) {
-          bool odd = false;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= not_finite16(lo[e]) || not_finite16(hi[e]);
-          if (__builtin_amdgcn_ballot_w64(odd)) {
-            s16x4 plus[2], minus[2], nan[2];
+        for (int k = 0; k < 2; ++k)
+          x[h][k] = ld_tr((const bf16 *)((const char *)vt + (r0 + 16 * h + 8 * k) * L::ROWB + (va ^ (64 * b))));
+      if constexpr (MASK) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd |= not_finite16(x[i / 8][i / 4 % 2][i % 4]);
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+          // infinities of each sign counted where the row sees them; no number counts as both
+          f32x16 plus, minus;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            s16x4 up[2], down[2];
             bf16x8 on;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const int w = (uint16_t)x[e / 4][e % 4];
-              plus[e / 4][e % 4] = w == 0x7f80 ? 0x3f80 : 0;
-              minus[e / 4][e % 4] = w == 0xff80 ? 0x3f80 : 0;
-              nan[e / 4][e % 4] = not_finite16(w) && (w & 0x7f) ? 0x3f80 : 0;
-              if (not_finite16(w)) x[e / 4][e % 4] = 0;
+              const int w = (uint16_t)x[h][e / 4][e % 4];
+              const bool out = not_finite16(w), nan = out && (w & 0x7f);
+              up[e / 4][e % 4] = nan || w == 0x7f80 ? 0x3f80 : 0;
+              down[e / 4][e % 4] = nan || w == 0xff80 ? 0x3f80 : 0;
+              if (out) x[h][e / 4][e % 4] = 0;
               on[e] = (float)pf[h][e] != 0.f ? f2bf(1.f) : f2bf(0.f);
             }
-            auto add = [&](const s16x4 (&ind)[2], float value) {
-              f32x16 n;
+            plus = mfma32(__builtin_bit_cast(bf16x8, up), on, plus);
+            minus = mfma32(__builtin_bit_cast(bf16x8, down), on, minus);
+          }
 #pragma unroll
-              for (int v = 0; v < 16; ++v) n[v] = 0.f;
-              n = mfma32(__builtin_bit_cast(bf16x8, ind), on, n);
-#pragma unroll
-              for (int v = 0; v < 16; ++v)
-                if (n[v] > 0.f) st.o[b][v] += value;
-            };
-            add(plus, INFINITY);
-            add(minus, -INFINITY);
-            add(nan, NAN);
+          for (int v = 0; v < 16; ++v) {
+            if (plus[v] > 0.f) st.o[b][v] += INFINITY;
+            if (minus[v] > 0.f) st.o[b][v] -= INFINITY;
           }
         }
-        st.o[b] = mfma32(__builtin_bit_cast(bf16x8, x), pf[h], st.o[b]);
       }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) st.o[b] = mfma32(__builtin_bit_cast(bf16x8, x[h]), pf[h], st.o[b]);
     }
   } else {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int r = r0 + 8 * (v / 4) + 4 * g + v % 4;
+    for (int b = 0; b < L::HB; ++b) {
+      float x[16];
 #pragma unroll
-      for (int b = 0; b < L::HB; ++b) {
-        float x = vt[r * HD + 32 * b + l32];
-        if constexpr (MASK) {
-          const bool odd = (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) == 0x7f800000u;
-          if (__builtin_amdgcn_ballot_w64(odd)) {
+      for (int v = 0; v < 16; ++v)
+        x[v] = *(const float *)((const char *)vt + (r0 + 8 * (v / 4) + v % 4) * L::ROWB + 128 * b + va);
+      if constexpr (MASK) {
+        bool odd = false;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) odd |= (__builtin_bit_cast(uint32_t, x[v]) & 0x7f800000u) == 0x7f800000u;
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+          f32x16 plus, minus;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
             const float on = p[v] != 0.f ? 1.f : 0.f;
-            auto add = [&](bool is, float value) {
-              f32x16 n;
+            plus = mfma32f(x[v] == INFINITY || x[v] != x[v] ? 1.f : 0.f, on, plus);
+            minus = mfma32f(x[v] == -INFINITY || x[v] != x[v] ? 1.f : 0.f, on, minus);
+            if (!(fabsf(x[v]) < INFINITY)) x[v] = 0.f;
+          }
 #pragma unroll
-              for (int w = 0; w < 16; ++w) n[w] = 0.f;
-              n = mfma32f(is ? 1.f : 0.f, on, n);
-#pragma unroll
-              for (int w = 0; w < 16; ++w)
-                if (n[w] > 0.f) st.o[b][w] += value;
-            };
-            add(x == INFINITY, INFINITY);
-            add(x == -INFINITY, -INFINITY);
-            add(x != x, NAN);
-            if (odd) x = 0.f;
+          for (int v = 0; v < 16; ++v) {
+            if (plus[v] > 0.f) st.o[b][v] += INFINITY;
+            if (minus[v] > 0.f) st.o[b][v] -= INFINITY;
           }
         }
-        st.o[b] = mfma32f(x, p[v], st.o[b]);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) st.o[b] = mfma32f(x[v], p[v], st.o[b]);
+    }
+  }
+}
+
+// NB blocks of 32 keys, key0 .. in LDS rows r0 ..: scores, probabilities, O += P V.
+// MASK: some row does not see some key of them.
+template <typename T, int HD, bool MASK, int NB>
+CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
+                    int lane, const Seen &seen) {
+  const int g = lane / 32;
+  f32x16 s[NB];
+  scores<T, HD, NB>(kt, r0, q, lane, s);
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb) {
+    if constexpr (MASK) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int key = key0 + 32 * kb + 8 * (v / 4) + 4 * g + v % 4;
+        bool hide = key < seen.lo || key > seen.hi;
+        if (seen.bad && !hide) hide = seen.pages[div_by(key, seen.ps_div) - seen.first] < 0;
+        if (hide) s[kb][v] = -INFINITY;
       }
     }
+    float p[16], sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      p[v] = fast_exp2(fmaf(s[kb][v], c, -st.ref));
+      sum += p[v];
+    }
+    if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {  // (also where the sum is no number)
+      float mx = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+      // only rows that need one: a row's result does not depend on the tile's others
+      const float other = __shfl_xor(sum, 32, 64);
+      const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
+      const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
+      const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
+      const float base = ref == -INFINITY ? 0.f : ref;
+      st.ref = ref;
+      st.l *= alpha;
+#pragma unroll
+      for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
+      sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        p[v] = fast_exp2(fmaf(s[kb][v], c, -base));
+        sum += p[v];
+      }
+    }
+    st.l += sum;
+    weigh<T, HD, MASK>(vt, r0 + 32 * kb, p, st, lane);
   }
 }
 
@@ -279,13 +319,21 @@ CRF_DEV void block32(const T *kt, const T *vt, int r0, int key0, const QFrag<T, 
 // work(t) = min(base + (t + 1) BM, cap) + over.
 struct SeqWork {
   int64_t base, cap, over;
-  int tiles, bm;
+  int tiles, below, bm;  // below: tiles under the ceiling
   __host__ __device__ int64_t before(int t) const {  // work of the tiles before t
-    const int64_t room = cap - base;
-    const int64_t k = room <= 0 ? 0 : room / bm < t ? room / bm : t;
+    const int64_t k = below < t ? below : t;
     return k * base + bm * (k * (k + 1) / 2) + (t - k) * cap + t * over;
   }
 };
+
+// floor(a / b) of 0 <= a < 2^62 and b > 0 with a quotient below 2^50 (in doubles, put
+// right by at most one: a tenth of the instructions of a 64-bit division)
+__host__ __device__ inline int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a / (double)b);
+  if (q * b > a) --q;
+  if (a - q * b >= b) ++q;
+  return q;
+}
 
 // A unit, or the part of one, that a workgroup computes.
 struct Task {
@@ -300,11 +348,17 @@ struct Shape {
   int G, nkv, window, bm, bkv;  // query heads of a KV head; rows and keys of a tile
 
   __host__ __device__ SeqWork work(int n, int len) const {
-    SeqWork w;
-    w.tiles = (int)(((int64_t)n * G + bm - 1) / bm);
+    SeqWork w;  // (rows of a sequence stay below 2^30)
+    w.tiles = (int)((unsigned)(n * G + bm - 1) / (unsigned)bm);
     w.bm = bm;
     w.base = (int64_t)(len - n) * G;
-    w.cap = window > 0 ? (int64_t)window * G + bm : INT64_MAX / 4;
+    w.cap = 0;
+    w.below = w.tiles;
+    if (window > 0) {
+      w.cap = (int64_t)window * G + bm;
+      const int64_t room = w.cap - w.base;
+      if (room < (int64_t)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
+    }
     w.over = (int64_t)bkv * G;
     return w;
   }
@@ -334,7 +388,7 @@ struct Shape {
   __host__ __device__ int64_t part_at(int64_t at, int64_t end, int64_t share, int wg, int64_t seq_base, Task &t) const {
     const SeqWork w = work(t.n, t.len);
     const int64_t one = w.before(w.tiles), off = at - seq_base;
-    t.kvh = (int)(off / one);
+    t.kvh = (int)quotient(off, one);
     const int64_t rem = off - t.kvh * one;
     int lo = 0, hi = w.tiles;
     while (hi - lo > 1) {
@@ -346,10 +400,10 @@ struct Shape {
     const int64_t u0 = seq_base + t.kvh * one + w.before(lo), cost = w.before(lo + 1) - w.before(lo), u1 = u0 + cost;
     const int64_t stop = u1 < end ? u1 : end;
     const int k0 = first_key(t) / bkv, k = last_key(t) / bkv + 1 - k0;
-    t.t0 = k0 + (int)((at - u0) * k / cost);
-    t.t1 = stop == u1 ? k0 + k : k0 + (int)((stop - u0) * k / cost);
-    t.owner = (int)(u0 / share);
-    t.parts = (int)((u1 - 1) / share) - t.owner + 1;
+    t.t0 = at == u0 ? k0 : k0 + (int)quotient((at - u0) * k, cost);
+    t.t1 = stop == u1 ? k0 + k : k0 + (int)quotient((stop - u0) * k, cost);
+    t.owner = (int)quotient(u0, share);
+    t.parts = (int)quotient(u1 - 1, share) - t.owner + 1;
     t.part = wg - t.owner;
     return stop;
   }
@@ -357,9 +411,10 @@ struct Shape {
 
 // Work of a workgroup when `total` is dealt out to at most `slots`, and how many get any.
 __host__ __device__ inline void deal(int64_t total, int64_t least, int slots, int64_t &share, int &n_wg) {
-  const int64_t want = total / least < 1 ? 1 : total / least < slots ? total / least : slots;
-  share = (total + want - 1) / want;
-  n_wg = (int)((total + share - 1) / share);
+  int64_t want = quotient(total, least);
+  want = want < 1 ? 1 : want < slots ? want : slots;
+  share = quotient(total + want - 1, want);
+  n_wg = (int)quotient(total + share - 1, share);
 }
 
 // Stretch of workgroup `bid`: neighbouring stretches, which share keys, lie on one
@@ -373,11 +428,26 @@ __host__ __device__ inline int stretch_of(int bid, int n_wg) {
 // and the one that begins in its stretch and goes on past it.
 __host__ __device__ inline int part_slot(int owner, int part) { return part == 0 ? 2 * owner + 1 : 2 * (owner + part); }
 
+// What the threads of a workgroup tell each other about the batch.
 template <int NT>
-struct Scan {
-  int64_t wsum[NT / 64];
+struct ScheduleLds {
+  int64_t sum[NT / 64], base;
+  int seq, start, n, len;
+};
+
+template <int NT>
+struct Schedule {
+  const PagedAttn &p;
+  ScheduleLds<NT> &lds;
+  Shape sh;
+  bool many;
+  int wg;
+  int64_t share, at, end;  // many: next unit and their number; else the stretch [at, end) of all work
+  int seq;                 // sequence that holds `at`, -1 before the first search
+  int64_t seq_base;        // where its work begins
+
   // exclusive prefix of v over the workgroup, *total the sum
-  CRF_DEV int64_t run(int64_t v, int64_t *total) {
+  CRF_DEV int64_t scan(int64_t v, int64_t *total) {
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
     int64_t x = v;
 #pragma unroll
@@ -386,62 +456,81 @@ struct Scan {
       if (lane >= o) x += y;
     }
     __syncthreads();
-    if (lane == 63) wsum[w] = x;
+    if (lane == 63) lds.sum[w] = x;
     __syncthreads();
-    int64_t at = 0, sum = 0;
+    int64_t before = 0, sum = 0;
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) {
-      if (i < w) at += wsum[i];
-      sum += wsum[i];
+      if (i < w) before += lds.sum[i];
+      sum += lds.sum[i];
     }
     *total = sum;
-    return at + x - v;
+    return before + x - v;
   }
-};
 
-template <int NT>
-struct Schedule {
-  const PagedAttn &p;
-  Scan<NT> &scan;
-  int &found;
-  int64_t &found_base;
-  Shape sh;
-  bool many;
-  int wg;
-  int64_t share, at, end;  // many: next unit and their number; else the stretch [at, end) of all work
-  int seq;                 // sequence that holds `at`, -1 before the first search
-  int64_t seq_base;        // where its work begins
+  CRF_DEV static int64_t uniform(int64_t v) {
+    return ((int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  }
+  CRF_DEV void hold(int s, int start, int n, int len, int64_t base) {
+    lds.seq = s;
+    lds.start = start;
+    lds.n = n;
+    lds.len = len;
+    lds.base = base;
+  }
+  CRF_DEV void take(Task &t) {
+    __syncthreads();
+    seq = __builtin_amdgcn_readfirstlane(lds.seq);
+    t.start = __builtin_amdgcn_readfirstlane(lds.start);
+    t.n = __builtin_amdgcn_readfirstlane(lds.n);
+    t.len = __builtin_amdgcn_readfirstlane(lds.len);
+    seq_base = uniform(lds.base);
+  }
 
-  // Sums the batch and takes this workgroup's stretch; false: nothing to do.
-  CRF_DEV bool begin(int slots) {
-    int64_t w = 0, u = 0, total_w, total_u;
+  // Sums the batch and takes this workgroup's stretch, with the sequence that it
+  // begins in when one pass sees all of them; false: nothing to do.  may_many: the
+  // units can be that many.
+  CRF_DEV bool begin(int slots, bool may_many) {
+    int64_t w = 0, u = 0, mine = 0, total;
+    int start = 0, len = 0, n = 0;
     for (int s = threadIdx.x; s < p.b.n_seqs; s += NT) {
-      int start, len;
-      const int n = seq_new(p.b, s, start, len);
+      n = seq_new(p.b, s, start, len);
       if (n == 0) continue;
-      w += sh.seq_work(n, len);
-      u += (int64_t)sh.work(n, len).tiles * sh.nkv;
+      mine = sh.seq_work(n, len);
+      w += mine;
+      if (may_many) u += (int64_t)sh.work(n, len).tiles * sh.nkv;
     }
-    (void)scan.run(w, &total_w);
-    (void)scan.run(u, &total_u);
-    many = slots == 0 || total_u >= (int64_t)MANY * slots;
+    many = false;
+    if (may_many) {
+      (void)scan(u, &total);
+      total = uniform(total);
+      many = total >= (int64_t)MANY * slots;
+    }
     seq = -1;
     if (many) {
       at = blockIdx.x;
-      end = total_u;
+      end = total;
       return at < end;
     }
-    if (total_w == 0) return false;
+    const int64_t before = scan(w, &total);
+    total = uniform(total);
+    if (total == 0) return false;
     int n_wg;
-    deal(total_w, (int64_t)MIN_KEYS * sh.G, slots, share, n_wg);
-    wg = stretch_of(blockIdx.x, n_wg);
+    deal(total, (int64_t)p.least_keys * sh.G, slots, share, n_wg);
+    share = uniform(share);
+    wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
     if (wg < 0) return false;
     at = wg * share;
-    end = at + share < total_w ? at + share : total_w;
+    end = at + share < total ? at + share : total;
+    if (p.b.n_seqs <= NT) {
+      if (w > 0 && at >= before && at < before + w) hold(threadIdx.x, start, n, len, before);
+      seq = -2;  // held, not taken yet
+    }
     return true;
   }
 
-  // Sequence that holds position x of the prefix sums of f(new tokens, length).
+  // Holds the sequence in which position x of the prefix sums of f(new tokens, length) lies.
   template <typename F>
   CRF_DEV void find(int64_t x, F f) {
     int64_t done = 0;
@@ -451,19 +540,11 @@ struct Schedule {
       const int n = s < p.b.n_seqs ? seq_new(p.b, s, start, len) : 0;
       const int64_t v = n > 0 ? f(n, len) : 0;
       int64_t total;
-      const int64_t b = done + scan.run(v, &total);
-      if (v > 0 && x >= b && x < b + v) {
-        found = s;
-        found_base = b;
-      }
+      const int64_t b = done + scan(v, &total);
+      if (v > 0 && x >= b && x < b + v) hold(s, start, n, len, b);
       done += total;
       if (x < done) break;
     }
-    __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(found);
-    const int64_t b = found_base;
-    seq_base = ((int64_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
-               (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
   }
 
   // The next task; false: done.
@@ -471,25 +552,27 @@ struct Schedule {
     if (at >= end) return false;
     if (many) {
       find(at, [&](int n, int len) { return (int64_t)sh.work(n, len).tiles * sh.nkv; });
+      take(t);
       t.seq = seq;
-      t.n = seq_new(p.b, seq, t.start, t.len);
       sh.whole(at - seq_base, t);
       at += gridDim.x;
-      return true;
-    }
-    if (seq < 0) {
-      find(at, [&](int n, int len) { return sh.seq_work(n, len); });
-      t.n = seq_new(p.b, seq, t.start, t.len);
     } else {
-      for (;; ++seq) {  // (`at` is before the end of all work, so some sequence holds it)
-        t.n = seq_new(p.b, seq, t.start, t.len);
-        const int64_t w = t.n > 0 ? sh.seq_work(t.n, t.len) : 0;
-        if (at < seq_base + w) break;
-        seq_base += w;
+      if (seq < 0) {
+        if (seq == -1) find(at, [&](int n, int len) { return sh.seq_work(n, len); });
+        take(t);
+      } else {
+        for (;; ++seq) {  // (`at` is before the end of all work, so some sequence holds it)
+          t.n = seq_new(p.b, seq, t.start, t.len);
+          const int64_t w = t.n > 0 ? sh.seq_work(t.n, t.len) : 0;
+          if (at < seq_base + w) break;
+          seq_base += w;
+        }
       }
+      t.seq = seq;
+      at = uniform(sh.part_at(at, end, share, wg, seq_base, t));
     }
-    t.seq = seq;
-    at = sh.part_at(at, end, share, wg, seq_base, t);
+    for (int *x : {&t.kvh, &t.tile, &t.start, &t.n, &t.len, &t.t0, &t.t1, &t.parts, &t.part, &t.owner})
+      *x = __builtin_amdgcn_readfirstlane(*x);
     return true;
   }
 };
@@ -541,14 +624,14 @@ CRF_DEV void join(const Writer<T, HD> &wr, const Task &t, float2 *ml, int &last)
   }
   __syncthreads();
   if (!last) return;
+  // the others' parts are in memory: no line of them may be left in a cache
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   const int step = ML_CAP / t.parts;  // rows joined at a time
   for (int r0 = 0; r0 < wr.rows; r0 += step) {
     const int rows = min(step, wr.rows - r0);
     for (int i = tid; i < rows * t.parts; i += NT) {
       const int part = i % t.parts, r = r0 + i / t.parts;
-      const uint64_t u = __hip_atomic_load((const uint64_t *)(wr.template part_row<BM>(part_slot(t.owner, part), r) + HD),
-                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      ml[i] = make_float2(__builtin_bit_cast(float, (uint32_t)u), __builtin_bit_cast(float, (uint32_t)(u >> 32)));
+      ml[i] = *(const float2 *)(wr.template part_row<BM>(part_slot(t.owner, part), r) + HD);
     }
     __syncthreads();
     for (int i = tid; i < rows * (HD / 4); i += NT) {
@@ -557,12 +640,15 @@ CRF_DEV void join(const Writer<T, HD> &wr, const Task &t, float2 *ml, int &last)
       float ref = -INFINITY, l = 0.f;
       for (int k = 0; k < t.parts; ++k) ref = fmaxf(ref, m[k].x);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
       for (int k = 0; k < t.parts; ++k) {
-        if (m[k].y == 0.f) continue;  // (a part of which the row sees nothing)
-        const float w = fast_exp2(m[k].x - ref);
+        // (a part of which the row sees nothing has no O)
+        const f32x4 x = *(const f32x4 *)(wr.template part_row<BM>(part_slot(t.owner, k), r0 + r) + e);
+        const bool some = m[k].y != 0.f;
+        const float w = some ? fast_exp2(m[k].x - ref) : 0.f;
         l += w * m[k].y;
-        o += w * ld_agent16(wr.template part_row<BM>(part_slot(t.owner, k), r0 + r) + e);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] = some ? fmaf(w, x[v], o[v]) : o[v];
       }
       wr.out4(r0 + r, e, o, ref, l);
     }
@@ -578,16 +664,27 @@ CRF_DEV void st_ml(float *p, float ref, float l) {
 
 // ---------------------------------------------------------------- keys and values from the pages
 
-// Stages page numbers and loads rows of keys and values.
-template <typename T, int HD, bool UNI>
+// Stages page numbers and loads rows of keys and values, ROWS a wave and tile.
+//
+// UNI (pages of a multiple of 16 tokens): groups of 16 rows share a page, whose base
+// goes into a buffer resource that ends where the sequence does; what lies past it,
+// and every row of a page out of range, arrives as zeros.  Else each lane finds its
+// own row's page, and the rows that nobody may read come from a block of zeros.
+template <typename T, int HD, bool UNI, int ROWS>
 struct Pages {
   using L = Layout<T, HD>;
+  static constexpr int GRP = ROWS < 16 ? ROWS : 16;
   const PagedBatch &b;
   const char *zeros;
-  int *pg;     // LDS, PGCAP numbers: logical page first + i
-  int *bad;    // LDS: some page of the unit is out of range
-  int first, len, kvh;
+  int *pg;   // LDS, PGCAP numbers: logical page first + i
+  int *bad;  // LDS: some page of the unit is out of range
+  int first, len, kvh, lds_row0, lane;
   const int32_t *table;
+
+  // A lane's bytes from the first of the rows that load i of a group covers (1 KiB).
+  CRF_DEV uint32_t kbytes(int i, uint32_t k0) const { return k0 ^ (((i * L::RPI) & (L::CH < 16 ? L::CH - 1 : 15)) * 16); }
+  // (V's slots repeat every 4 rows: RPI is a multiple of that wherever it has any)
+  static_assert(sizeof(T) == 4 || L::RPI % 4 == 0, "V rows of a load");
 
   CRF_DEV void fill(int page, int end_key, int nt) {  // pages page .. that hold keys before end_key
     first = page;
@@ -603,46 +700,42 @@ struct Pages {
     }
   }
 
-  // ROWS keys from key0 on (a multiple of ROWS) to LDS rows lds_row0 ..; keys past the
-  // sequence and on pages out of range arrive as zeros.  Always 2 * ROWS / RPI loads.
-  template <int ROWS>
-  CRF_DEV void load(int key0, T *kdst, T *vdst, int lds_row0, int lane) const {
-    const int lrow = lane / L::CH, lslot = lane % L::CH;
-    constexpr int GRP = ROWS < 16 ? ROWS : 16;  // rows that share a page when page_size % 16 == 0
+  // Keys key0 .. (a multiple of ROWS): always 2 * ROWS / RPI loads.
+  CRF_DEV void load(int key0, T *kdst, T *vdst) const {
+    const int lrow = lane / L::CH;
+    uint32_t k0 = lrow * L::ROWB + L::kslot(lds_row0 + lrow, lane % L::CH) * 16;
+    uint32_t v0 = lrow * L::ROWB + L::vslot(lrow, lane % L::CH) * 16;
+    fresh(k0);
+    fresh(v0);
 #pragma unroll
     for (int g0 = 0; g0 < ROWS; g0 += GRP) {
       const int kg = key0 + g0;
-      bool whole = false;
-      int64_t off = 0;
-      if (UNI) {
-        const int lp = div_by(kg, b.ps_div);
-        const int q = kg < len ? __builtin_amdgcn_readfirstlane(pg[lp - first]) : -1;
-        whole = q >= 0 && kg + GRP <= len;
-        off = (int64_t)q * b.page_bytes + ((int64_t)kvh * b.page_size + (kg - lp * b.page_size)) * L::ROWB;
-      }
-      if (whole) {
-        const char *kb = b.k + off, *vb = b.v + off;
+      char *kl = (char *)kdst + (lds_row0 + g0) * L::ROWB, *vl = (char *)vdst + (lds_row0 + g0) * L::ROWB;
+      if constexpr (UNI) {
+        const int lp = div_by(kg, b.ps_div), rows = min(len - kg, GRP);
+        const int q = rows > 0 ? __builtin_amdgcn_readfirstlane(pg[lp - first]) : -1;
+        const int64_t off =
+            q < 0 ? 0 : q * b.page_bytes + (int64_t)(kvh * b.page_size + kg - lp * b.page_size) * L::ROWB;
+        const uint32_t bytes = q < 0 ? 0 : rows * L::ROWB;
+        const __amdgpu_buffer_rsrc_t kr = make_rsrc(b.k + off, bytes), vr = make_rsrc(b.v + off, bytes);
 #pragma unroll
-        for (int i = 0; i < GRP; i += L::RPI) {
-          const int row = i + lrow, tr = lds_row0 + g0 + row;
-          gload16(kb + (uint32_t)(row * L::ROWB + L::kslot(tr, lslot) * 16), kdst + (lds_row0 + g0 + i) * HD);
-          gload16(vb + (uint32_t)(row * L::ROWB + L::vslot(tr, lslot) * 16), vdst + (lds_row0 + g0 + i) * HD);
+        for (int i = 0; i < GRP / L::RPI; ++i) {
+          dma16(kr, (lds_char *)(kl + i * 1024), kbytes(i, k0) + i * 1024, 0);
+          dma16(vr, (lds_char *)(vl + i * 1024), v0 + i * 1024, 0);
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < GRP; i += L::RPI) {
-          const int row = i + lrow, tr = lds_row0 + g0 + row, key = kg + row;
+        for (int i = 0; i < GRP / L::RPI; ++i) {
+          const int key = kg + i * L::RPI + lrow;
           int q = -1, slot = 0;
           if (key < len) {
             const int lp = div_by(key, b.ps_div);
             q = pg[lp - first];
             slot = key - lp * b.page_size;
           }
-          const int64_t o = (int64_t)q * b.page_bytes + ((int64_t)kvh * b.page_size + slot) * L::ROWB;
-          const char *kp = q >= 0 ? b.k + o + L::kslot(tr, lslot) * 16 : zeros;
-          const char *vp = q >= 0 ? b.v + o + L::vslot(tr, lslot) * 16 : zeros;
-          gload16(kp, kdst + (lds_row0 + g0 + i) * HD);
-          gload16(vp, vdst + (lds_row0 + g0 + i) * HD);
+          const int64_t o = q * b.page_bytes + (int64_t)(kvh * b.page_size + slot - lrow) * L::ROWB;
+          gload16(q >= 0 ? b.k + o + kbytes(i, k0) : zeros, kl + i * 1024);
+          gload16(q >= 0 ? b.v + o + v0 : zeros, vl + i * 1024);
         }
       }
     }
@@ -652,23 +745,25 @@ struct Pages {
 // ---------------------------------------------------------------- tiles of 128 rows
 
 template <typename T, int HD, bool UNI>
-__global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots) {
+__global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots, bool may_many) {
   using L = Layout<T, HD>;
   constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW, BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * HD;
+  // one array per stage and operand, so that the compiler sees that loads into one
+  // stage do not touch the other
   __shared__ __align__(16) T ks0[TILE], ks1[TILE], vs0[TILE], vs1[TILE];
   __shared__ int pg[PGCAP];
-  __shared__ int bad, last, found;
-  __shared__ int64_t found_base;
-  __shared__ Scan<NT> scan;
+  __shared__ int bad, last;
+  __shared__ ScheduleLds<NT> slds;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, scan, found, found_base, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
-  if (!sch.begin(slots)) return;
+  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
+  if (!sch.begin(slots, may_many)) return;
   const int G = sch.sh.G;
+  const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
   Task t;
   while (sch.next(t)) {
-    const int rows = min((int64_t)BM, (int64_t)t.n * G - (int64_t)t.tile * BM);
+    const int rows = min(BM, t.n * G - t.tile * BM);
     const Writer<T, HD> wr{p, t, G, t.tile * BM, rows};
     const int base = t.len - t.n;
     // this lane's row (padding rows repeat the last one)
@@ -680,16 +775,21 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
     q.load((const T *)p.q + (int64_t)(t.start + tok) * p.q_ld + head * HD, g);
     RowState<HD> st;
     st.clear();
-    Pages<T, HD, UNI> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, p.b.tables + (int64_t)t.seq * p.b.table_stride};
-    const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
+    Pages<T, HD, UNI, BKV / NW> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, wave * (BKV / NW), lane,
+                                      p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
     __syncthreads();  // the task before has left LDS
     if (tid == 0) bad = 0;
     __syncthreads();
     const int end_key = t.t1 * BKV;
-
-    auto tile = [&](int it, const T *kt, const T *vt, T *kn, T *vn) {
+    if (t.t0 < t.t1) {
+      pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
+      __syncthreads();
+      pages.load(t.t0 * BKV + wave * (BKV / NW), ks0, vs0);
+    }
+    for (int it = t.t0; it < t.t1; ++it) {
       const int kt0 = it * BKV;
+      const bool second = (it - t.t0) & 1;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       if (it + 1 < t.t1) {
@@ -697,29 +797,22 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
           pages.fill(div_by(kt0, p.b.ps_div), end_key, NT);
           __syncthreads();
         }
-        pages.template load<BKV / NW>(kt0 + BKV + wave * (BKV / NW), kn, vn, wave * (BKV / NW), lane);
+        if (second)
+          pages.load(kt0 + BKV + wave * (BKV / NW), ks0, vs0);
+        else
+          pages.load(kt0 + BKV + wave * (BKV / NW), ks1, vs1);
       }
-      if (wave * 32 >= rows || kt0 > pos_hi || kt0 + BKV <= first_seen) return;
+      if (wave * 32 >= rows || kt0 > pos_hi || kt0 + BKV <= first_seen) continue;
       const Seen seen{pos > far ? pos - far : 0, pos, bad != 0, pg, pages.first, p.b.ps_div};
-      if (kt0 + BKV - 1 > pos_lo || kt0 < last_first || bad) {
-#pragma unroll
+      if (kt0 + BKV - 1 > pos_lo || kt0 < last_first || seen.bad) {
+#pragma unroll 1
         for (int kb = 0; kb < BKV; kb += 32)
-          block32<T, HD, true>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+          blocks<T, HD, true, 1>(second ? ks1 : ks0, second ? vs1 : vs0, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+      } else if (second) {
+        blocks<T, HD, false, BKV / 32>(ks1, vs1, 0, kt0, q, st, p.scale_log2, lane, seen);
       } else {
-#pragma unroll
-        for (int kb = 0; kb < BKV; kb += 32)
-          block32<T, HD, false>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+        blocks<T, HD, false, BKV / 32>(ks0, vs0, 0, kt0, q, st, p.scale_log2, lane, seen);
       }
-    };
-
-    if (t.t0 < t.t1) {
-      pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
-      __syncthreads();
-      pages.template load<BKV / NW>(t.t0 * BKV + wave * (BKV / NW), ks0, vs0, wave * (BKV / NW), lane);
-    }
-    for (int it = t.t0; it < t.t1; it += 2) {
-      tile(it, ks0, vs0, ks1, vs1);
-      if (it + 1 < t.t1) tile(it + 1, ks1, vs1, ks0, vs0);
     }
 
     const float l = st.l + __shfl_xor(st.l, 32, 64);
@@ -757,25 +850,26 @@ struct KeysCfg {
 };
 
 template <typename T, int HD, bool UNI>
-__global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW)) void attn_keys_kernel(const PagedAttn p, int slots) {
+__global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_CU)) void attn_keys_kernel(
+    const PagedAttn p, int slots, bool may_many) {
   using L = Layout<T, HD>;
   constexpr int NW = KeysCfg<T, HD>::NW, NT = 64 * NW, BM = 32, BKV = 32 * NW, TILE = BKV * HD;
   constexpr int LOADS = 2 * 32 / L::RPI;  // of a wave's stage
   __shared__ __align__(16) T ks0[TILE], ks1[TILE], vs0[TILE], vs1[TILE];
   __shared__ int pg[PGCAP];
   __shared__ float2 wml[NW][32];
-  __shared__ int bad, last, found;
-  __shared__ int64_t found_base;
-  __shared__ Scan<NT> scan;
+  __shared__ int bad, last;
+  __shared__ ScheduleLds<NT> slds;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, scan, found, found_base, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
-  if (!sch.begin(slots)) return;
+  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
+  if (!sch.begin(slots, may_many)) return;
   const int G = sch.sh.G;
+  const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
   Task t;
   while (sch.next(t)) {
-    const int rows = min((int64_t)BM, (int64_t)t.n * G - (int64_t)t.tile * BM);
+    const int rows = min(BM, t.n * G - t.tile * BM);
     const Writer<T, HD> wr{p, t, G, t.tile * BM, rows};
     const int base = t.len - t.n;
     const int row = t.tile * BM + min(l32, rows - 1);
@@ -785,8 +879,8 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW)) void attn_keys_kernel(co
     q.load((const T *)p.q + (int64_t)(t.start + tok) * p.q_ld + head * HD, g);
     RowState<HD> st;
     st.clear();
-    Pages<T, HD, UNI> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, p.b.tables + (int64_t)t.seq * p.b.table_stride};
-    const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
+    Pages<T, HD, UNI, 32> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, wave * 32, lane,
+                                p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
     __syncthreads();
     if (tid == 0) bad = 0;
@@ -799,30 +893,34 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW)) void attn_keys_kernel(co
       const int z = keys / BKV < t.t1 ? (int)(keys / BKV) : t.t1;
       pages.fill(fp, z * BKV, NT);
       __syncthreads();
-      const bool odd = bad != 0;
-      const Seen seen{pos > far ? pos - far : 0, pos, odd, pg, fp, p.b.ps_div};
-      auto load = [&](int it, T *k, T *v) { pages.template load<32>(it * BKV + wave * 32, k, v, wave * 32, lane); };
-      auto step = [&](int it, T *k, T *v) {
+      const Seen seen{pos > far ? pos - far : 0, pos, bad != 0, pg, fp, p.b.ps_div};
+      pages.load(a * BKV + wave * 32, ks0, vs0);
+      if (a + 1 < z) pages.load((a + 1) * BKV + wave * 32, ks1, vs1);
+      for (int it = a; it < z; ++it) {
+        const bool second = (it - a) & 1;
+        // the wave's loads of this tile; those of the next one stay in flight
         if (it + 1 < z)
           asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         else
           asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const int key0 = it * BKV + wave * 32;
         if (key0 <= pos_hi && key0 + 32 > first_seen) {
-          if (key0 + 31 > pos_lo || key0 < last_first || odd)
-            block32<T, HD, true>(k, v, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+          if (key0 + 31 > pos_lo || key0 < last_first || seen.bad)
+            blocks<T, HD, true, 1>(second ? ks1 : ks0, second ? vs1 : vs0, wave * 32, key0, q, st, p.scale_log2, lane,
+                                   seen);
+          else if (second)
+            blocks<T, HD, false, 1>(ks1, vs1, wave * 32, key0, q, st, p.scale_log2, lane, seen);
           else
-            block32<T, HD, false>(k, v, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+            blocks<T, HD, false, 1>(ks0, vs0, wave * 32, key0, q, st, p.scale_log2, lane, seen);
         }
         // the stage is read before it is loaded again
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (it + 2 < z) load(it + 2, k, v);
-      };
-      load(a, ks0, vs0);
-      if (a + 1 < z) load(a + 1, ks1, vs1);
-      for (int it = a; it < z; it += 2) {
-        step(it, ks0, vs0);
-        if (it + 1 < z) step(it + 1, ks1, vs1);
+        if (it + 2 < z) {
+          if (second)
+            pages.load((it + 2) * BKV + wave * 32, ks1, vs1);
+          else
+            pages.load((it + 2) * BKV + wave * 32, ks0, vs0);
+        }
       }
       a = z;
       __syncthreads();
@@ -872,11 +970,12 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW)) void attn_keys_kernel(co
 }
 
 template <typename T, int HD, bool UNI>
-hipError_t launch(hipStream_t s, const PagedAttn &p) {
+hipError_t launch(hipStream_t s, PagedAttn p) {
   const int G = p.nq / p.nkv;
   // up to 32 rows to a sequence and KV head: the keys are shared out
   const bool keys = (int64_t)p.b.max_new * G <= 32;
   const int bm = keys ? 32 : 128;
+  p.least_keys = sizeof(T) == 2 ? 256 : 64;
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
   const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 4)) : 0;  // two slots a workgroup
   int slots = (int)(room < resident ? room : resident);
@@ -884,13 +983,14 @@ hipError_t launch(hipStream_t s, const PagedAttn &p) {
   slots = slots / 8 * 8;
   // (a sequence's last tile may be short)
   const int64_t most = ((int64_t)p.b.n_rows * G / bm + p.b.n_seqs) * p.nkv;
-  const int64_t grid = most < (int64_t)MANY * slots ? slots : most;
+  const bool may_many = most >= (int64_t)MANY * slots;
+  const int64_t grid = may_many ? most : slots;
   if (grid < 1) return hipSuccess;
   const dim3 g((unsigned)(grid < (1 << 24) ? grid : 1 << 24));
   if (keys)
-    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots);
+    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots, may_many);
   else
-    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI>), g, dim3(256), 0, s, p, slots);
+    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI>), g, dim3(256), 0, s, p, slots, may_many);
   return hipGetLastError();
 }
 
