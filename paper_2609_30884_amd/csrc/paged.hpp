@@ -89,7 +89,8 @@ struct PagedAttn {
   unsigned *tickets;   // PAGED_TICKETS, zero between launches
   const char *zeros;   // PAGED_ZERO_BYTES
   int n_cu;
-  int least_keys;      // keys that are worth a workgroup (set by the launcher)
+  int least_keys;      // keys that are worth a workgroup (set by the launcher, as g_div)
+  FastDiv g_div;       // by nq / nkv
 };
 hipError_t launch_paged_attn(hipStream_t s, bool f32, const PagedAttn &p);
 

@@ -107,7 +107,7 @@ struct QFrag {
 // The keys that a lane's row sees: [lo, hi]; bad: some pages of the unit are out of
 // range, whose keys nobody sees.
 struct Seen {
-  int lo, hi;
+  int lo, hi, end;  // end: of the sequence
   bool bad;
   const int *pages;  // staged page numbers, the first of logical page `first`
   int first;
@@ -118,6 +118,14 @@ template <int HD>
 struct RowState {
   f32x16 o[HD / 32];
   float ref, l;
+  CRF_DEV bool finite() const {
+    float z = 0.f;
+#pragma unroll
+    for (int b = 0; b < HD / 32; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) z = fmaf(o[b][v], 0.f, z);
+    return z == 0.f;
+  }
   CRF_DEV void clear() {
 #pragma unroll
     for (int b = 0; b < HD / 32; ++b)
@@ -127,8 +135,6 @@ struct RowState {
     l = 0.f;
   }
 };
-
-CRF_DEV bool not_finite16(int h) { return (h & 0x7f80) == 0x7f80; }
 
 // Raw scores of NB blocks of 32 keys (LDS rows r0 ..) against the wave's 32 rows.
 // bf16: the K fragments are read two steps ahead of the products that use them (the
@@ -166,15 +172,31 @@ CRF_DEV void scores(const T *kt, int r0, const QFrag<T, HD> &q, int lane, f32x16
   }
 }
 
-// O += P V for the probabilities p of 32 keys in LDS rows r0 ...  MASK: a value that
-// is not finite takes no part in a row that does not see its key (p = 0), though the
-// product multiplies it by zero: such values are taken out of the product and added
-// where the weight is not zero.
-template <typename T, int HD, bool MASK>
+// How a block of keys is taken.  ALL: every row sees all of it.  SOME: some row does
+// not see some key.  CAREFUL: the same where a value that is not finite may belong to
+// a key that some row does not see: the product would multiply it by that row's
+// weight zero, so such values are taken out of the product and added where the weight
+// is not zero.  (Units run with SOME first, and again if their result is not finite.)
+enum Take { ALL, SOME, CAREFUL };
+
+// O += P V for the probabilities p of 32 keys in LDS rows r0 ...
+template <typename T, int HD, Take TAKE>
 CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, int lane) {
   using L = Layout<T, HD>;
   uint32_t va = L::vaddr(lane);
   fresh(va);
+  // infinities of each sign counted where the row sees them; no number counts as both
+  f32x16 plus, minus;
+  auto settle = [&](f32x16 &o) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      if (plus[v] > 0.f) o[v] += INFINITY;
+      if (minus[v] > 0.f) o[v] -= INFINITY;
+    }
+  };
+  if constexpr (TAKE == CAREFUL)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
   if constexpr (sizeof(T) == 2) {
     bf16x8 pf[2];
 #pragma unroll
@@ -190,37 +212,27 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           x[h][k] = ld_tr((const bf16 *)((const char *)vt + (r0 + 16 * h + 8 * k) * L::ROWB + (va ^ (64 * b))));
-      if constexpr (MASK) {
-        bool odd = false;
+      if constexpr (TAKE == CAREFUL) {
+        f32x16 zero;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) odd |= not_finite16(x[i / 8][i / 4 % 2][i % 4]);
-        if (__builtin_amdgcn_ballot_w64(odd)) {
-          // infinities of each sign counted where the row sees them; no number counts as both
-          f32x16 plus, minus;
+        for (int v = 0; v < 16; ++v) zero[v] = 0.f;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
+        for (int h = 0; h < 2; ++h) {
+          s16x4 up[2], down[2];
+          bf16x8 on;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            s16x4 up[2], down[2];
-            bf16x8 on;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int w = (uint16_t)x[h][e / 4][e % 4];
-              const bool out = not_finite16(w), nan = out && (w & 0x7f);
-              up[e / 4][e % 4] = nan || w == 0x7f80 ? 0x3f80 : 0;
-              down[e / 4][e % 4] = nan || w == 0xff80 ? 0x3f80 : 0;
-              if (out) x[h][e / 4][e % 4] = 0;
-              on[e] = (float)pf[h][e] != 0.f ? f2bf(1.f) : f2bf(0.f);
-            }
-            plus = mfma32(__builtin_bit_cast(bf16x8, up), on, plus);
-            minus = mfma32(__builtin_bit_cast(bf16x8, down), on, minus);
+          for (int e = 0; e < 8; ++e) {
+            const int w = (uint16_t)x[h][e / 4][e % 4];
+            const bool out = (w & 0x7f80) == 0x7f80, nan = out && (w & 0x7f);
+            up[e / 4][e % 4] = nan || w == 0x7f80 ? 0x3f80 : 0;
+            down[e / 4][e % 4] = nan || w == 0xff80 ? 0x3f80 : 0;
+            if (out) x[h][e / 4][e % 4] = 0;
+            on[e] = (float)pf[h][e] != 0.f ? f2bf(1.f) : f2bf(0.f);
           }
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            if (plus[v] > 0.f) st.o[b][v] += INFINITY;
-            if (minus[v] > 0.f) st.o[b][v] -= INFINITY;
-          }
+          plus = mfma32(__builtin_bit_cast(bf16x8, up), on, h == 0 ? zero : plus);
+          minus = mfma32(__builtin_bit_cast(bf16x8, down), on, h == 0 ? zero : minus);
         }
+        settle(st.o[b]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) st.o[b] = mfma32(__builtin_bit_cast(bf16x8, x[h]), pf[h], st.o[b]);
@@ -232,27 +244,17 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         x[v] = *(const float *)((const char *)vt + (r0 + 8 * (v / 4) + v % 4) * L::ROWB + 128 * b + va);
-      if constexpr (MASK) {
-        bool odd = false;
+      if constexpr (TAKE == CAREFUL) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) odd |= (__builtin_bit_cast(uint32_t, x[v]) & 0x7f800000u) == 0x7f800000u;
-        if (__builtin_amdgcn_ballot_w64(odd)) {
-          f32x16 plus, minus;
+        for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const float on = p[v] != 0.f ? 1.f : 0.f;
-            plus = mfma32f(x[v] == INFINITY || x[v] != x[v] ? 1.f : 0.f, on, plus);
-            minus = mfma32f(x[v] == -INFINITY || x[v] != x[v] ? 1.f : 0.f, on, minus);
-            if (!(fabsf(x[v]) < INFINITY)) x[v] = 0.f;
-          }
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            if (plus[v] > 0.f) st.o[b][v] += INFINITY;
-            if (minus[v] > 0.f) st.o[b][v] -= INFINITY;
-          }
+        for (int v = 0; v < 16; ++v) {
+          const float on = p[v] != 0.f ? 1.f : 0.f;
+          plus = mfma32f(x[v] == INFINITY || x[v] != x[v] ? 1.f : 0.f, on, plus);
+          minus = mfma32f(x[v] == -INFINITY || x[v] != x[v] ? 1.f : 0.f, on, minus);
+          if (!(fabsf(x[v]) < INFINITY)) x[v] = 0.f;
         }
+        settle(st.o[b]);
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) st.o[b] = mfma32f(x[v], p[v], st.o[b]);
@@ -261,8 +263,7 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
 }
 
 // NB blocks of 32 keys, key0 .. in LDS rows r0 ..: scores, probabilities, O += P V.
-// MASK: some row does not see some key of them.
-template <typename T, int HD, bool MASK, int NB>
+template <typename T, int HD, Take TAKE, int NB>
 CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
                     int lane, const Seen &seen) {
   const int g = lane / 32;
@@ -270,13 +271,21 @@ CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, H
   scores<T, HD, NB>(kt, r0, q, lane, s);
 #pragma unroll
   for (int kb = 0; kb < NB; ++kb) {
-    if constexpr (MASK) {
+    if constexpr (TAKE != ALL) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = key0 + 32 * kb + 8 * (v / 4) + 4 * g + v % 4;
-        bool hide = key < seen.lo || key > seen.hi;
-        if (seen.bad && !hide) hide = seen.pages[div_by(key, seen.ps_div) - seen.first] < 0;
-        if (hide) s[kb][v] = -INFINITY;
+        if (key < seen.lo || key > seen.hi) s[kb][v] = -INFINITY;
+      }
+      if (seen.bad) {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i) {  // keys of pages out of range
+          const int key = key0 + 32 * kb + i;
+          if (key < seen.end && seen.pages[div_by(key, seen.ps_div) - seen.first] < 0)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (8 * (v / 4) + 4 * g + v % 4 == i) s[kb][v] = -INFINITY;
+        }
       }
     }
     float p[16], sum = 0.f;
@@ -308,7 +317,7 @@ CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, H
       }
     }
     st.l += sum;
-    weigh<T, HD, MASK>(vt, r0 + 32 * kb, p, st, lane);
+    weigh<T, HD, TAKE>(vt, r0 + 32 * kb, p, st, lane);
   }
 }
 
@@ -317,21 +326,23 @@ CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, H
 // Row tiles of a sequence and their work in key x row units, a straight line in the
 // tile (its keys end where its tokens do) up to a ceiling given by the window:
 // work(t) = min(base + (t + 1) BM, cap) + over.
+//
+// Work is counted in doubles: whole numbers below 2^53, exact, with instructions of
+// their own where 64-bit integers take many.
 struct SeqWork {
-  int64_t base, cap, over;
+  double base, cap, over;
   int tiles, below, bm;  // below: tiles under the ceiling
-  __host__ __device__ int64_t before(int t) const {  // work of the tiles before t
-    const int64_t k = below < t ? below : t;
-    return k * base + bm * (k * (k + 1) / 2) + (t - k) * cap + t * over;
+  __host__ __device__ double before(int t) const {  // work of the tiles before t
+    const double k = below < t ? below : t;
+    return k * base + bm * (k * (k + 1) * 0.5) + (t - k) * cap + t * over;
   }
 };
 
-// floor(a / b) of 0 <= a < 2^62 and b > 0 with a quotient below 2^50 (in doubles, put
-// right by at most one: a tenth of the instructions of a 64-bit division)
-__host__ __device__ inline int64_t quotient(int64_t a, int64_t b) {
-  int64_t q = (int64_t)((double)a / (double)b);
-  if (q * b > a) --q;
-  if (a - q * b >= b) ++q;
+// floor(a / b) for whole a >= 0, b > 0
+__host__ __device__ inline double quotient(double a, double b) {
+  double q = floor(a / b);
+  if (q * b > a) q -= 1;
+  if (a - q * b >= b) q += 1;
   return q;
 }
 
@@ -346,38 +357,42 @@ struct Task {
 
 struct Shape {
   int G, nkv, window, bm, bkv;  // query heads of a KV head; rows and keys of a tile
+  FastDiv g_div;                // by G
 
+  __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
   __host__ __device__ SeqWork work(int n, int len) const {
     SeqWork w;  // (rows of a sequence stay below 2^30)
     w.tiles = (int)((unsigned)(n * G + bm - 1) / (unsigned)bm);
     w.bm = bm;
-    w.base = (int64_t)(len - n) * G;
+    w.base = (double)(len - n) * G;
     w.cap = 0;
     w.below = w.tiles;
     if (window > 0) {
-      w.cap = (int64_t)window * G + bm;
-      const int64_t room = w.cap - w.base;
-      if (room < (int64_t)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
+      w.cap = (double)window * G + bm;
+      const double room = w.cap - w.base;
+      if (room < (double)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
     }
-    w.over = (int64_t)bkv * G;
+    w.over = (double)bkv * G;
     return w;
   }
-  __host__ __device__ int64_t seq_work(int n, int len) const {
+  // All of a sequence's work, or (units) its units.
+  __host__ __device__ double seq_work(int n, int len, bool units = false) const {
     const SeqWork w = work(n, len);
-    return w.before(w.tiles) * nkv;
+    return (units ? (double)w.tiles : w.before(w.tiles)) * nkv;
   }
   __host__ __device__ int first_key(const Task &t) const {  // of the tile's first row
-    const int pos = t.len - t.n + (int)((int64_t)t.tile * bm / G);
+    const int pos = t.len - t.n + by_g(t.tile * bm);
     return window > 0 && pos >= window ? pos - window + 1 : 0;
   }
   __host__ __device__ int last_key(const Task &t) const {  // of the tile's last row
-    const int64_t r = ((int64_t)t.tile + 1) * bm, rows = (int64_t)t.n * G;
-    return t.len - t.n + (int)(((r < rows ? r : rows) - 1) / G);
+    const int r = (t.tile + 1) * bm, rows = t.n * G;
+    return t.len - t.n + by_g((r < rows ? r : rows) - 1);
   }
   // Unit i of the sequence's, whole: longest first, its KV heads next to each other.
-  __host__ __device__ void whole(int64_t i, Task &t) const {
-    t.kvh = (int)(i % nkv);
-    t.tile = work(t.n, t.len).tiles - 1 - (int)(i / nkv);
+  __host__ __device__ void whole(int i, Task &t) const {
+    const int k = i / nkv;
+    t.kvh = i - k * nkv;
+    t.tile = work(t.n, t.len).tiles - 1 - k;
     t.t0 = first_key(t) / bkv;
     t.t1 = last_key(t) / bkv + 1;
     t.parts = 1;
@@ -385,22 +400,25 @@ struct Shape {
   // What workgroup wg, whose stretch ends at `end`, computes from position `at` of
   // all work on, `at` being in the sequence, whose work begins at seq_base; returns
   // where it stops (the end of the unit or of the stretch).
-  __host__ __device__ int64_t part_at(int64_t at, int64_t end, int64_t share, int wg, int64_t seq_base, Task &t) const {
+  __host__ __device__ double part_at(double at, double end, double share, int wg, double seq_base, Task &t) const {
     const SeqWork w = work(t.n, t.len);
-    const int64_t one = w.before(w.tiles), off = at - seq_base;
+    const double one = w.before(w.tiles), off = at - seq_base;
     t.kvh = (int)quotient(off, one);
-    const int64_t rem = off - t.kvh * one;
+    const double rem = off - t.kvh * one;
     int lo = 0, hi = w.tiles;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if (w.before(mid) <= rem) lo = mid;
       else hi = mid;
     }
     t.tile = lo;
-    const int64_t u0 = seq_base + t.kvh * one + w.before(lo), cost = w.before(lo + 1) - w.before(lo), u1 = u0 + cost;
-    const int64_t stop = u1 < end ? u1 : end;
+    const double first = w.before(lo), cost = w.before(lo + 1) - first, u0 = seq_base + t.kvh * one + first,
+                 u1 = u0 + cost;
+    const double stop = u1 < end ? u1 : end;
     const int k0 = first_key(t) / bkv, k = last_key(t) / bkv + 1 - k0;
-    t.t0 = at == u0 ? k0 : k0 + (int)quotient((at - u0) * k, cost);
+    // (both neighbours of a border find it by the same arithmetic)
+    t.t0 = k0 + (int)quotient((at - u0) * k, cost);
     t.t1 = stop == u1 ? k0 + k : k0 + (int)quotient((stop - u0) * k, cost);
     t.owner = (int)quotient(u0, share);
     t.parts = (int)quotient(u1 - 1, share) - t.owner + 1;
@@ -410,8 +428,8 @@ struct Shape {
 };
 
 // Work of a workgroup when `total` is dealt out to at most `slots`, and how many get any.
-__host__ __device__ inline void deal(int64_t total, int64_t least, int slots, int64_t &share, int &n_wg) {
-  int64_t want = quotient(total, least);
+__host__ __device__ inline void deal(double total, double least, int slots, double &share, int &n_wg) {
+  double want = quotient(total, least);
   want = want < 1 ? 1 : want < slots ? want : slots;
   share = quotient(total + want - 1, want);
   n_wg = (int)quotient(total + share - 1, share);
@@ -431,148 +449,109 @@ __host__ __device__ inline int part_slot(int owner, int part) { return part == 0
 // What the threads of a workgroup tell each other about the batch.
 template <int NT>
 struct ScheduleLds {
-  int64_t sum[NT / 64], base;
+  double sum[NT / 64], base;
   int seq, start, n, len;
 };
+
+CRF_DEV double uniform(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 |
+                                        (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
 
 template <int NT>
 struct Schedule {
   const PagedAttn &p;
   ScheduleLds<NT> &lds;
   Shape sh;
-  bool many;
-  int wg;
-  int64_t share, at, end;  // many: next unit and their number; else the stretch [at, end) of all work
-  int seq;                 // sequence that holds `at`, -1 before the first search
-  int64_t seq_base;        // where its work begins
+  int slots;
+  bool many;          // units dealt out whole
+  bool dealt = false;
+  int wg = 0;
+  double share = 0, at = -1, end = 0;  // many: next unit and their number; else the stretch [at, end) of all work
 
-  // exclusive prefix of v over the workgroup, *total the sum
-  CRF_DEV int64_t scan(int64_t v, int64_t *total) {
+  // Prefix sums over the sequences of their work (units: of their units), of which the
+  // total is returned; the sequence that holds position x is left in LDS.
+  CRF_DEV double pass(double x, bool units) {
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
-    int64_t x = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = __shfl_up(x, o, 64);
-      if (lane >= o) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) lds.sum[w] = x;
-    __syncthreads();
-    int64_t before = 0, sum = 0;
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) {
-      if (i < w) before += lds.sum[i];
-      sum += lds.sum[i];
-    }
-    *total = sum;
-    return before + x - v;
-  }
-
-  CRF_DEV static int64_t uniform(int64_t v) {
-    return ((int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
-  }
-  CRF_DEV void hold(int s, int start, int n, int len, int64_t base) {
-    lds.seq = s;
-    lds.start = start;
-    lds.n = n;
-    lds.len = len;
-    lds.base = base;
-  }
-  CRF_DEV void take(Task &t) {
-    __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(lds.seq);
-    t.start = __builtin_amdgcn_readfirstlane(lds.start);
-    t.n = __builtin_amdgcn_readfirstlane(lds.n);
-    t.len = __builtin_amdgcn_readfirstlane(lds.len);
-    seq_base = uniform(lds.base);
-  }
-
-  // Sums the batch and takes this workgroup's stretch, with the sequence that it
-  // begins in when one pass sees all of them; false: nothing to do.  may_many: the
-  // units can be that many.
-  CRF_DEV bool begin(int slots, bool may_many) {
-    int64_t w = 0, u = 0, mine = 0, total;
-    int start = 0, len = 0, n = 0;
-    for (int s = threadIdx.x; s < p.b.n_seqs; s += NT) {
-      n = seq_new(p.b, s, start, len);
-      if (n == 0) continue;
-      mine = sh.seq_work(n, len);
-      w += mine;
-      if (may_many) u += (int64_t)sh.work(n, len).tiles * sh.nkv;
-    }
-    many = false;
-    if (may_many) {
-      (void)scan(u, &total);
-      total = uniform(total);
-      many = total >= (int64_t)MANY * slots;
-    }
-    seq = -1;
-    if (many) {
-      at = blockIdx.x;
-      end = total;
-      return at < end;
-    }
-    const int64_t before = scan(w, &total);
-    total = uniform(total);
-    if (total == 0) return false;
-    int n_wg;
-    deal(total, (int64_t)p.least_keys * sh.G, slots, share, n_wg);
-    share = uniform(share);
-    wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
-    if (wg < 0) return false;
-    at = wg * share;
-    end = at + share < total ? at + share : total;
-    if (p.b.n_seqs <= NT) {
-      if (w > 0 && at >= before && at < before + w) hold(threadIdx.x, start, n, len, before);
-      seq = -2;  // held, not taken yet
-    }
-    return true;
-  }
-
-  // Holds the sequence in which position x of the prefix sums of f(new tokens, length) lies.
-  template <typename F>
-  CRF_DEV void find(int64_t x, F f) {
-    int64_t done = 0;
+    double done = 0;
+#pragma unroll 1
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += NT) {
       const int s = s0 + threadIdx.x;
-      int start, len;
+      int start = 0, len = 0;
       const int n = s < p.b.n_seqs ? seq_new(p.b, s, start, len) : 0;
-      const int64_t v = n > 0 ? f(n, len) : 0;
-      int64_t total;
-      const int64_t b = done + scan(v, &total);
-      if (v > 0 && x >= b && x < b + v) hold(s, start, n, len, b);
-      done += total;
-      if (x < done) break;
+      const double v = n > 0 ? sh.seq_work(n, len, units) : 0;
+      double sum = v;
+#pragma unroll 1
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += y;
+      }
+      __syncthreads();
+      if (lane == 63) lds.sum[w] = sum;
+      __syncthreads();
+      double base = done + sum - v;
+#pragma unroll
+      for (int i = 0; i < NT / 64; ++i) {
+        if (i < w) base += lds.sum[i];
+        done += lds.sum[i];
+      }
+      if (v > 0 && x >= base && x < base + v) {
+        lds.seq = s;
+        lds.start = start;
+        lds.n = n;
+        lds.len = len;
+        lds.base = base;
+      }
     }
+    __syncthreads();
+    return uniform(done);
   }
 
   // The next task; false: done.
   CRF_DEV bool next(Task &t) {
-    if (at >= end) return false;
+#pragma unroll 1
+    for (;;) {
+      if (dealt && __builtin_amdgcn_readfirstlane(at >= end)) return false;
+      const double total = pass(at, many);
+      if (dealt) break;
+      if (many && total < (double)MANY * slots) {  // not that many
+        many = false;
+        continue;
+      }
+      dealt = true;
+      if (many) {
+        at = blockIdx.x;
+        end = total;
+        continue;
+      }
+      if (__builtin_amdgcn_readfirstlane(total == 0)) return false;
+      int n_wg;
+      deal(total, (double)p.least_keys * sh.G, slots, share, n_wg);
+      share = uniform(share);
+      wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
+      if (wg < 0) return false;
+      at = wg * share;
+      end = at + share < total ? at + share : total;
+    }
+    t.seq = __builtin_amdgcn_readfirstlane(lds.seq);
+    t.start = __builtin_amdgcn_readfirstlane(lds.start);
+    t.n = __builtin_amdgcn_readfirstlane(lds.n);
+    t.len = __builtin_amdgcn_readfirstlane(lds.len);
+    const double base = uniform(lds.base);
     if (many) {
-      find(at, [&](int n, int len) { return (int64_t)sh.work(n, len).tiles * sh.nkv; });
-      take(t);
-      t.seq = seq;
-      sh.whole(at - seq_base, t);
+      sh.whole(__builtin_amdgcn_readfirstlane((int)(at - base)), t);
       at += gridDim.x;
     } else {
-      if (seq < 0) {
-        if (seq == -1) find(at, [&](int n, int len) { return sh.seq_work(n, len); });
-        take(t);
-      } else {
-        for (;; ++seq) {  // (`at` is before the end of all work, so some sequence holds it)
-          t.n = seq_new(p.b, seq, t.start, t.len);
-          const int64_t w = t.n > 0 ? sh.seq_work(t.n, t.len) : 0;
-          if (at < seq_base + w) break;
-          seq_base += w;
-        }
-      }
-      t.seq = seq;
-      at = uniform(sh.part_at(at, end, share, wg, seq_base, t));
+      at = uniform(sh.part_at(at, end, share, wg, base, t));
     }
-    for (int *x : {&t.kvh, &t.tile, &t.start, &t.n, &t.len, &t.t0, &t.t1, &t.parts, &t.part, &t.owner})
-      *x = __builtin_amdgcn_readfirstlane(*x);
+    t.kvh = __builtin_amdgcn_readfirstlane(t.kvh);
+    t.tile = __builtin_amdgcn_readfirstlane(t.tile);
+    t.t0 = __builtin_amdgcn_readfirstlane(t.t0);
+    t.t1 = __builtin_amdgcn_readfirstlane(t.t1);
+    t.parts = __builtin_amdgcn_readfirstlane(t.parts);
+    t.part = __builtin_amdgcn_readfirstlane(t.part);
+    t.owner = __builtin_amdgcn_readfirstlane(t.owner);
     return true;
   }
 };
@@ -581,27 +560,27 @@ template <typename T, int HD>
 struct Writer {
   const PagedAttn &p;
   const Task &t;
-  int G, row0, rows;  // first row of the tile and its rows
+  const Shape &sh;
+  int rows;  // of the tile
 
-  CRF_DEV void locate(int r, int64_t &token, int &head) const {
-    const int a = row0 + r;
-    token = t.start + a / G;
-    head = t.kvh * G + a % G;
-  }
-  // four elements from e on of the tile's row r: o / l, and the row's log-sum
-  CRF_DEV void out4(int r, int e, f32x4 o, float ref, float l) const {
-    int64_t token;
-    int head;
-    locate(r, token, head);
+  // Row r of the tile: its token and head, o / l from element e on (NF groups of 4
+  // elements, 8 apart), and the row's log-sum.
+  template <int NF>
+  CRF_DEV void out(int r, int e, const f32x4 (&o)[NF], float ref, float l) const {
+    const int a = t.tile * sh.bm + r, k = sh.by_g(a), head = t.kvh * sh.G + a - k * sh.G;
+    const int64_t token = t.start + k;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T *dst = (T *)p.out + token * p.out_ld + head * HD + e;
-    o *= inv;
-    if constexpr (sizeof(T) == 2)
-      st8(dst, pack_bf16x4(o[0], o[1], o[2], o[3]));
-    else
-      *reinterpret_cast<f32x4 *>(dst) = o;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const f32x4 x = o[i] * inv;
+      if constexpr (sizeof(T) == 2)
+        st8(dst + 8 * i, pack_bf16x4(x[0], x[1], x[2], x[3]));
+      else
+        *reinterpret_cast<f32x4 *>(dst + 8 * i) = x;
+    }
     if (e == 0 && p.lse)
-      p.lse[token * p.nq + head] = l == 0.f ? -INFINITY : 0.69314718055994531f * (ref + log2f(l));
+      p.lse[token * p.nq + head] = l == 0.f ? -INFINITY : 0.69314718055994531f * (ref + __builtin_amdgcn_logf(l));
   }
   template <int BM>
   CRF_DEV float *part_row(int slot, int r) const {
@@ -640,7 +619,7 @@ CRF_DEV void join(const Writer<T, HD> &wr, const Task &t, float2 *ml, int &last)
       float ref = -INFINITY, l = 0.f;
       for (int k = 0; k < t.parts; ++k) ref = fmaxf(ref, m[k].x);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
+#pragma unroll 4
       for (int k = 0; k < t.parts; ++k) {
         // (a part of which the row sees nothing has no O)
         const f32x4 x = *(const f32x4 *)(wr.template part_row<BM>(part_slot(t.owner, k), r0 + r) + e);
@@ -650,7 +629,8 @@ CRF_DEV void join(const Writer<T, HD> &wr, const Task &t, float2 *ml, int &last)
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] = some ? fmaf(w, x[v], o[v]) : o[v];
       }
-      wr.out4(r0 + r, e, o, ref, l);
+      const f32x4 one[1] = {o};
+      wr.out(r0 + r, e, one, ref, l);
     }
     __syncthreads();
   }
@@ -757,83 +737,88 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
-  if (!sch.begin(slots, may_many)) return;
-  const int G = sch.sh.G;
+  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, p.g_div}, slots, may_many};
+  const Shape &sh = sch.sh;
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
   Task t;
+#pragma unroll 1
   while (sch.next(t)) {
-    const int rows = min(BM, t.n * G - t.tile * BM);
-    const Writer<T, HD> wr{p, t, G, t.tile * BM, rows};
-    const int base = t.len - t.n;
+    const int rows = min(BM, t.n * sh.G - t.tile * BM);
+    const Writer<T, HD> wr{p, t, sh, rows};
+    const int base = t.len - t.n, row0 = t.tile * BM;
     // this lane's row (padding rows repeat the last one)
-    const int r = wave * 32 + l32, row = t.tile * BM + min(r, rows - 1);
-    const int tok = row / G, head = t.kvh * G + row % G, pos = base + tok;
-    const int pos_lo = base + (t.tile * BM + min(wave * 32, rows - 1)) / G;
-    const int pos_hi = base + (t.tile * BM + min(wave * 32 + 31, rows - 1)) / G;
+    const int r = wave * 32 + l32, row = row0 + min(r, rows - 1);
+    const int tok = sh.by_g(row), head = t.kvh * sh.G + row - tok * sh.G, pos = base + tok;
+    const int pos_lo = base + sh.by_g(row0 + min(wave * 32, rows - 1));
+    const int pos_hi = base + sh.by_g(row0 + min(wave * 32 + 31, rows - 1));
     QFrag<T, HD> q;
     q.load((const T *)p.q + (int64_t)(t.start + tok) * p.q_ld + head * HD, g);
     RowState<HD> st;
-    st.clear();
     Pages<T, HD, UNI, BKV / NW> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, wave * (BKV / NW), lane,
                                       p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
-    __syncthreads();  // the task before has left LDS
-    if (tid == 0) bad = 0;
-    __syncthreads();
     const int end_key = t.t1 * BKV;
-    if (t.t0 < t.t1) {
-      pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
-      __syncthreads();
-      pages.load(t.t0 * BKV + wave * (BKV / NW), ks0, vs0);
-    }
-    for (int it = t.t0; it < t.t1; ++it) {
-      const int kt0 = it * BKV;
-      const bool second = (it - t.t0) & 1;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (it + 1 < t.t1) {
-        if (div_by(min(kt0 + 2 * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
-          pages.fill(div_by(kt0, p.b.ps_div), end_key, NT);
-          __syncthreads();
-        }
-        if (second)
-          pages.load(kt0 + BKV + wave * (BKV / NW), ks0, vs0);
-        else
-          pages.load(kt0 + BKV + wave * (BKV / NW), ks1, vs1);
-      }
-      if (wave * 32 >= rows || kt0 > pos_hi || kt0 + BKV <= first_seen) continue;
-      const Seen seen{pos > far ? pos - far : 0, pos, bad != 0, pg, pages.first, p.b.ps_div};
-      if (kt0 + BKV - 1 > pos_lo || kt0 < last_first || seen.bad) {
+    if (tid == 0) bad = 0;
+    bool careful = false;
 #pragma unroll 1
-        for (int kb = 0; kb < BKV; kb += 32)
-          blocks<T, HD, true, 1>(second ? ks1 : ks0, second ? vs1 : vs0, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
-      } else if (second) {
-        blocks<T, HD, false, BKV / 32>(ks1, vs1, 0, kt0, q, st, p.scale_log2, lane, seen);
-      } else {
-        blocks<T, HD, false, BKV / 32>(ks0, vs0, 0, kt0, q, st, p.scale_log2, lane, seen);
+    for (;;) {
+      st.clear();
+      __syncthreads();  // the task (or the pass) before has left LDS
+      if (t.t0 < t.t1) {
+        pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
+        __syncthreads();
+        pages.load(t.t0 * BKV + wave * (BKV / NW), ks0, vs0);
       }
+#pragma unroll 1
+      for (int it = t.t0; it < t.t1; ++it) {
+        const int kt0 = it * BKV;
+        const bool second = (it - t.t0) & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (it + 1 < t.t1) {
+          if (div_by(min(kt0 + 2 * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
+            pages.fill(div_by(kt0, p.b.ps_div), end_key, NT);
+            __syncthreads();
+          }
+          if (second)
+            pages.load(kt0 + BKV + wave * (BKV / NW), ks0, vs0);
+          else
+            pages.load(kt0 + BKV + wave * (BKV / NW), ks1, vs1);
+        }
+        if (wave * 32 >= rows || kt0 > pos_hi || kt0 + BKV <= first_seen) continue;
+        const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, pages.first, p.b.ps_div};
+        if (kt0 + BKV - 1 > pos_lo || kt0 < last_first || seen.bad) {
+          const T *kt = second ? ks1 : ks0, *vt = second ? vs1 : vs0;
+#pragma unroll 1
+          for (int kb = 0; kb < BKV; kb += 32)
+            if (careful)
+              blocks<T, HD, CAREFUL, 1>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+            else
+              blocks<T, HD, SOME, 1>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+        } else if (second) {
+          blocks<T, HD, ALL, BKV / 32>(ks1, vs1, 0, kt0, q, st, p.scale_log2, lane, seen);
+        } else {
+          blocks<T, HD, ALL, BKV / 32>(ks0, vs0, 0, kt0, q, st, p.scale_log2, lane, seen);
+        }
+      }
+      if (careful || !__syncthreads_or(!st.finite())) break;
+      careful = true;
     }
 
     const float l = st.l + __shfl_xor(st.l, 32, 64);
+    f32x4 o[4 * L::HB];
+#pragma unroll
+    for (int i = 0; i < 4 * L::HB; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[i][v] = st.o[i / 4][4 * (i % 4) + v];
     if (t.parts == 1) {
-      if (r < rows)
-#pragma unroll
-        for (int b = 0; b < L::HB; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            wr.out4(r, 32 * b + 8 * i + 4 * g,
-                    f32x4{st.o[b][4 * i], st.o[b][4 * i + 1], st.o[b][4 * i + 2], st.o[b][4 * i + 3]}, st.ref, l);
+      if (r < rows) wr.out(r, 4 * g, o, st.ref, l);
       continue;
     }
     if (r < rows) {
       float *dst = wr.template part_row<BM>(part_slot(t.owner, t.part), r);
 #pragma unroll
-      for (int b = 0; b < L::HB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          st_agent16(dst + 32 * b + 8 * i + 4 * g,
-                     f32x4{st.o[b][4 * i], st.o[b][4 * i + 1], st.o[b][4 * i + 2], st.o[b][4 * i + 3]});
+      for (int i = 0; i < 4 * L::HB; ++i) st_agent16(dst + 8 * i + 4 * g, o[i]);
       if (g == 0) st_ml(dst + HD, st.ref, l);
     }
     join<T, HD, BM, NT>(wr, t, (float2 *)vs0, last);
@@ -863,67 +848,78 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV}};
-  if (!sch.begin(slots, may_many)) return;
-  const int G = sch.sh.G;
+  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, p.g_div}, slots, may_many};
+  const Shape &sh = sch.sh;
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
   Task t;
+#pragma unroll 1
   while (sch.next(t)) {
-    const int rows = min(BM, t.n * G - t.tile * BM);
-    const Writer<T, HD> wr{p, t, G, t.tile * BM, rows};
-    const int base = t.len - t.n;
-    const int row = t.tile * BM + min(l32, rows - 1);
-    const int tok = row / G, head = t.kvh * G + row % G, pos = base + tok;
-    const int pos_lo = base + t.tile * BM / G, pos_hi = base + (t.tile * BM + rows - 1) / G;
+    const int rows = min(BM, t.n * sh.G - t.tile * BM);
+    const Writer<T, HD> wr{p, t, sh, rows};
+    const int base = t.len - t.n, row0 = t.tile * BM;
+    const int row = row0 + min(l32, rows - 1);
+    const int tok = sh.by_g(row), head = t.kvh * sh.G + row - tok * sh.G, pos = base + tok;
+    const int pos_lo = base + sh.by_g(row0), pos_hi = base + sh.by_g(row0 + rows - 1);
     QFrag<T, HD> q;
     q.load((const T *)p.q + (int64_t)(t.start + tok) * p.q_ld + head * HD, g);
     RowState<HD> st;
-    st.clear();
     Pages<T, HD, UNI, 32> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, wave * 32, lane,
                                 p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
-    __syncthreads();
     if (tid == 0) bad = 0;
-    __syncthreads();
-
-    // stretches of tiles whose pages fit the staged table
-    for (int a = t.t0; a < t.t1;) {
-      const int fp = div_by(a * BKV, p.b.ps_div);
-      const int64_t keys = ((int64_t)fp + PGCAP) * p.b.page_size;  // end of the staged pages
-      const int z = keys / BKV < t.t1 ? (int)(keys / BKV) : t.t1;
-      pages.fill(fp, z * BKV, NT);
-      __syncthreads();
-      const Seen seen{pos > far ? pos - far : 0, pos, bad != 0, pg, fp, p.b.ps_div};
-      pages.load(a * BKV + wave * 32, ks0, vs0);
-      if (a + 1 < z) pages.load((a + 1) * BKV + wave * 32, ks1, vs1);
-      for (int it = a; it < z; ++it) {
-        const bool second = (it - a) & 1;
-        // the wave's loads of this tile; those of the next one stay in flight
-        if (it + 1 < z)
-          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-        else
-          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const int key0 = it * BKV + wave * 32;
-        if (key0 <= pos_hi && key0 + 32 > first_seen) {
-          if (key0 + 31 > pos_lo || key0 < last_first || seen.bad)
-            blocks<T, HD, true, 1>(second ? ks1 : ks0, second ? vs1 : vs0, wave * 32, key0, q, st, p.scale_log2, lane,
-                                   seen);
-          else if (second)
-            blocks<T, HD, false, 1>(ks1, vs1, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+    bool careful = false;
+#pragma unroll 1
+    for (;;) {
+      st.clear();
+      __syncthreads();  // the task (or the pass) before has left LDS
+      // stretches of tiles whose pages fit the staged table
+#pragma unroll 1
+      for (int a = t.t0; a < t.t1;) {
+        const int fp = div_by(a * BKV, p.b.ps_div);
+        // (whole tiles before the end of the staged pages)
+        const int64_t tiles = ((int64_t)fp + PGCAP) * p.b.page_size / BKV;
+        const int z = tiles < t.t1 ? (int)tiles : t.t1;
+        pages.fill(fp, z * BKV, NT);
+        __syncthreads();
+        const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, fp, p.b.ps_div};
+        pages.load(a * BKV + wave * 32, ks0, vs0);
+        if (a + 1 < z) pages.load((a + 1) * BKV + wave * 32, ks1, vs1);
+#pragma unroll 1
+        for (int it = a; it < z; ++it) {
+          const bool second = (it - a) & 1;
+          // the wave's loads of this tile; those of the next one stay in flight
+          if (it + 1 < z)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
           else
-            blocks<T, HD, false, 1>(ks0, vs0, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          const int key0 = it * BKV + wave * 32;
+          if (key0 <= pos_hi && key0 + 32 > first_seen) {
+            if (key0 + 31 > pos_lo || key0 < last_first || seen.bad) {
+              const T *kt = second ? ks1 : ks0, *vt = second ? vs1 : vs0;
+              if (careful)
+                blocks<T, HD, CAREFUL, 1>(kt, vt, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+              else
+                blocks<T, HD, SOME, 1>(kt, vt, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+            } else if (second) {
+              blocks<T, HD, ALL, 1>(ks1, vs1, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+            } else {
+              blocks<T, HD, ALL, 1>(ks0, vs0, wave * 32, key0, q, st, p.scale_log2, lane, seen);
+            }
+          }
+          // the stage is read before it is loaded again
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (it + 2 < z) {
+            if (second)
+              pages.load((it + 2) * BKV + wave * 32, ks1, vs1);
+            else
+              pages.load((it + 2) * BKV + wave * 32, ks0, vs0);
+          }
         }
-        // the stage is read before it is loaded again
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (it + 2 < z) {
-          if (second)
-            pages.load((it + 2) * BKV + wave * 32, ks1, vs1);
-          else
-            pages.load((it + 2) * BKV + wave * 32, ks0, vs0);
-        }
+        a = z;
+        __syncthreads();
       }
-      a = z;
-      __syncthreads();
+      if (careful || !__syncthreads_or(!st.finite())) break;
+      careful = true;
     }
 
     // join the waves: O of wave w at 32 x HD floats w of ks0 and ks1
@@ -958,7 +954,8 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         o += k * osum(w)[r * (HD / 4) + (c4 ^ (r & 15))];
       }
       if (t.parts == 1) {
-        wr.out4(r, 4 * c4, o, ref, l);
+        const f32x4 one[1] = {o};
+        wr.out(r, 4 * c4, one, ref, l);
       } else {
         float *dst = wr.template part_row<BM>(part_slot(t.owner, t.part), r);
         st_agent16(dst + 4 * c4, o);
@@ -976,6 +973,7 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   const bool keys = (int64_t)p.b.max_new * G <= 32;
   const int bm = keys ? 32 : 128;
   p.least_keys = sizeof(T) == 2 ? 256 : 64;
+  p.g_div = fast_div(G);
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
   const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 4)) : 0;  // two slots a workgroup
   int slots = (int)(room < resident ? room : resident);

@@ -26,11 +26,12 @@ int main() {
   for (int it = 0; it < 4000; ++it) {
     const int nkv = 1 + upto(7), G = 1 + upto(8), bm = it % 2 ? 32 : 128;
     const int window = upto(3) ? 0 : 1 + upto(3000);
-    const Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64};
+    const Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, fast_div(G)};
     const int slots = 8 * (1 + upto(63)), seqs = 1 + upto(40);
     const int most_new = bm == 32 ? (32 / G > 0 ? 32 / G : 1) : 1 + upto(1 + upto(2000));
     std::vector<int> n(seqs), len(seqs);
-    int64_t total = 0, units = 0;
+    double total = 0;
+    int64_t units = 0;
     for (int s = 0; s < seqs; ++s) {
       n[s] = upto(9) ? upto(most_new) : 0;
       len[s] = n[s] + upto(upto(3) ? 500 : 20000);
@@ -64,9 +65,9 @@ int main() {
     if (seen != units) return fail("number of units", it);
     if (total == 0) continue;
     // dealt out
-    int64_t share;
+    double share;
     int n_wg;
-    deal(total, (int64_t)256 * G, slots, share, n_wg);
+    deal(total, 256.0 * G, slots, share, n_wg);
     if (n_wg < 1 || n_wg > slots) return fail("more workgroups than slots", it);
     std::set<int> stretches;
     for (int b = 0; b < slots; ++b) {
@@ -77,13 +78,13 @@ int main() {
     std::map<std::tuple<int, int, int>, std::vector<Task>> unit;
     std::set<int> slot, owner;
     for (int wg = 0; wg < n_wg; ++wg) {
-      int64_t at = wg * share;
-      const int64_t end = std::min(at + share, total);
+      double at = wg * share;
+      const double end = std::min(at + share, total);
       while (at < end) {
-        int64_t base = 0;
+        double base = 0;
         int s = 0;
         for (;; ++s) {
-          const int64_t w = n[s] > 0 ? sh.seq_work(n[s], len[s]) : 0;
+          const double w = n[s] > 0 ? sh.seq_work(n[s], len[s]) : 0;
           if (at < base + w) break;
           base += w;
         }
@@ -91,7 +92,7 @@ int main() {
         t.seq = s;
         t.n = n[s];
         t.len = len[s];
-        const int64_t stop = sh.part_at(at, end, share, wg, base, t);
+        const double stop = sh.part_at(at, end, share, wg, base, t);
         if (stop <= at || stop > end) return fail("no progress", it);
         at = stop;
         unit[{s, t.kvh, t.tile}].push_back(t);
