@@ -43,8 +43,7 @@ namespace {
 
 constexpr float PSUM_MAX = 256.0f;  // a lane's sum of a block's probabilities that needs no new reference
 constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
-constexpr int ML_CAP = 2048;        // (reference, sum) pairs that a join holds in LDS
-constexpr int MANY = 4;             // units per resident workgroup from which none is split
+constexpr int MANY = 3;             // units per resident workgroup from which none is split
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -357,6 +356,7 @@ struct Task {
 
 struct Shape {
   int G, nkv, window, bm, bkv;  // query heads of a KV head; rows and keys of a tile
+  int over;                     // keys that a unit costs besides its own
   FastDiv g_div;                // by G
 
   __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
@@ -372,7 +372,7 @@ struct Shape {
       const double room = w.cap - w.base;
       if (room < (double)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
     }
-    w.over = (double)bkv * G;
+    w.over = (double)over * G;
     return w;
   }
   // All of a sequence's work, or (units) its units.
@@ -427,10 +427,13 @@ struct Shape {
   }
 };
 
-// Work of a workgroup when `total` is dealt out to at most `slots`, and how many get any.
-__host__ __device__ inline void deal(double total, double least, int slots, double &share, int &n_wg) {
+// Work of a workgroup when `total` is dealt out to at most `slots`, and how many get
+// any: no fewer than `heads` (the sequences' KV heads, which need not wait for each
+// other) and as many as have `least` each.
+__host__ __device__ inline void deal(double total, double least, int heads, int slots, double &share, int &n_wg) {
   double want = quotient(total, least);
-  want = want < 1 ? 1 : want < slots ? want : slots;
+  want = want < heads ? heads : want;
+  want = want < slots ? want : slots;
   share = quotient(total + want - 1, want);
   n_wg = (int)quotient(total + share - 1, share);
 }
@@ -446,104 +449,119 @@ __host__ __device__ inline int stretch_of(int bid, int n_wg) {
 // and the one that begins in its stretch and goes on past it.
 __host__ __device__ inline int part_slot(int owner, int part) { return part == 0 ? 2 * owner + 1 : 2 * (owner + part); }
 
-// What the threads of a workgroup tell each other about the batch.
-template <int NT>
-struct ScheduleLds {
-  double sum[NT / 64], base;
-  int seq, start, n, len;
-};
-
-CRF_DEV double uniform(double v) {
+// The value of lane `from` in every lane (a wave-uniform value).
+CRF_DEV int lane_value(int v, int from) { return __builtin_amdgcn_readlane(v, from); }
+CRF_DEV double lane_value(double v, int from) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 |
-                                        (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_value((int)(u >> 32), from) << 32 |
+                                        (uint32_t)lane_value((int)u, from));
 }
 
-template <int NT>
+// What a workgroup computes, unit after unit.  Every wave works it out for itself,
+// 64 sequences at a time, so that nothing waits for a barrier.
 struct Schedule {
   const PagedAttn &p;
-  ScheduleLds<NT> &lds;
   Shape sh;
   int slots;
-  bool many;          // units dealt out whole
+  bool many;  // units dealt out whole, gridDim.x apart; else stretches of work
   bool dealt = false;
   int wg = 0;
   double share = 0, at = -1, end = 0;  // many: next unit and their number; else the stretch [at, end) of all work
+  int seq = -1, start = 0, n = 0, len = 0;  // the sequence that holds `at` ...
+  double base = 0, work = 0;                // ... and where its work begins, and how much it is
+
+  struct Lane {  // a lane's sequence, its work and where that begins
+    int s, start, n, len;
+    double v, from;
+  };
 
   // Prefix sums over the sequences of their work (units: of their units), of which the
-  // total is returned; the sequence that holds position x is left in LDS.
-  CRF_DEV double pass(double x, bool units) {
-    const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
+  // total is returned; finds the sequence that holds position x, and leaves each lane
+  // its last sequence.
+  CRF_DEV double pass(double x, bool units, Lane &q) {
+    const int lane = threadIdx.x % 64;
     double done = 0;
 #pragma unroll 1
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += NT) {
-      const int s = s0 + threadIdx.x;
-      int start = 0, len = 0;
-      const int n = s < p.b.n_seqs ? seq_new(p.b, s, start, len) : 0;
-      const double v = n > 0 ? sh.seq_work(n, len, units) : 0;
-      double sum = v;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += 64) {
+      q.s = s0 + lane;
+      q.start = q.len = 0;
+      q.n = q.s < p.b.n_seqs ? seq_new(p.b, q.s, q.start, q.len) : 0;
+      q.v = q.n > 0 ? sh.seq_work(q.n, q.len, units) : 0;
+      double sum = q.v;
 #pragma unroll 1
       for (int o = 1; o < 64; o <<= 1) {
         const double y = __shfl_up(sum, o, 64);
         if (lane >= o) sum += y;
       }
-      __syncthreads();
-      if (lane == 63) lds.sum[w] = sum;
-      __syncthreads();
-      double base = done + sum - v;
-#pragma unroll
-      for (int i = 0; i < NT / 64; ++i) {
-        if (i < w) base += lds.sum[i];
-        done += lds.sum[i];
-      }
-      if (v > 0 && x >= base && x < base + v) {
-        lds.seq = s;
-        lds.start = start;
-        lds.n = n;
-        lds.len = len;
-        lds.base = base;
-      }
+      q.from = done + sum - q.v;
+      hold(x, q);
+      done += lane_value(sum, 63);
     }
-    __syncthreads();
-    return uniform(done);
+    return done;
+  }
+
+  CRF_DEV void hold(double x, const Lane &q) {
+    const uint64_t m = __builtin_amdgcn_ballot_w64(q.v > 0 && x >= q.from && x < q.from + q.v);
+    if (m) {
+      const int l = __builtin_ctzll(m);
+      seq = lane_value(q.s, l);
+      start = lane_value(q.start, l);
+      n = lane_value(q.n, l);
+      len = lane_value(q.len, l);
+      base = lane_value(q.from, l);
+      work = lane_value(q.v, l);
+    }
   }
 
   // The next task; false: done.
   CRF_DEV bool next(Task &t) {
-#pragma unroll 1
-    for (;;) {
-      if (dealt && __builtin_amdgcn_readfirstlane(at >= end)) return false;
-      const double total = pass(at, many);
-      if (dealt) break;
+    if (!dealt) {
+      dealt = true;
+      Lane q;
+      double total = pass(-1, many, q);
       if (many && total < (double)MANY * slots) {  // not that many
         many = false;
-        continue;
+        total = pass(-1, false, q);
       }
-      dealt = true;
       if (many) {
         at = blockIdx.x;
         end = total;
-        continue;
+      } else {
+        if (__builtin_amdgcn_readfirstlane(total == 0)) return false;
+        int n_wg;
+        deal(total, (double)p.least_keys * sh.G, p.b.n_seqs * sh.nkv, slots, share, n_wg);
+        share = lane_value(share, 0);
+        wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
+        if (wg < 0) return false;
+        at = wg * share;
+        end = at + share < total ? at + share : total;
+        if (p.b.n_seqs <= 64)  // the pass has seen them all
+          hold(at, q);
+        else
+          pass(at, false, q);
       }
-      if (__builtin_amdgcn_readfirstlane(total == 0)) return false;
-      int n_wg;
-      deal(total, (double)p.least_keys * sh.G, slots, share, n_wg);
-      share = uniform(share);
-      wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
-      if (wg < 0) return false;
-      at = wg * share;
-      end = at + share < total ? at + share : total;
     }
-    t.seq = __builtin_amdgcn_readfirstlane(lds.seq);
-    t.start = __builtin_amdgcn_readfirstlane(lds.start);
-    t.n = __builtin_amdgcn_readfirstlane(lds.n);
-    t.len = __builtin_amdgcn_readfirstlane(lds.len);
-    const double base = uniform(lds.base);
+    if (__builtin_amdgcn_readfirstlane(at >= end)) return false;
+    if (many) {
+      Lane q;
+      pass(at, true, q);
+    } else {
+#pragma unroll 1
+      while (__builtin_amdgcn_readfirstlane(at >= base + work)) {  // (some sequence holds `at`)
+        base += work;
+        n = seq_new(p.b, ++seq, start, len);
+        work = n > 0 ? sh.seq_work(n, len) : 0;
+      }
+    }
+    t.seq = __builtin_amdgcn_readfirstlane(seq);
+    t.start = __builtin_amdgcn_readfirstlane(start);
+    t.n = __builtin_amdgcn_readfirstlane(n);
+    t.len = __builtin_amdgcn_readfirstlane(len);
     if (many) {
       sh.whole(__builtin_amdgcn_readfirstlane((int)(at - base)), t);
       at += gridDim.x;
     } else {
-      at = uniform(sh.part_at(at, end, share, wg, base, t));
+      at = lane_value(sh.part_at(at, end, share, wg, base, t), 0);
     }
     t.kvh = __builtin_amdgcn_readfirstlane(t.kvh);
     t.tile = __builtin_amdgcn_readfirstlane(t.tile);
@@ -582,65 +600,80 @@ struct Writer {
     if (e == 0 && p.lse)
       p.lse[token * p.nq + head] = l == 0.f ? -INFINITY : 0.69314718055994531f * (ref + __builtin_amdgcn_logf(l));
   }
-  template <int BM>
-  CRF_DEV float *part_row(int slot, int r) const {
-    return p.part + ((int64_t)slot * BM + r) * (HD + 4);
+};
+
+// Partials of unit parts, 2 a workgroup: BM x HD floats, and behind all of them BM
+// pairs (reference, sum).  They are stored past the caches of the XCD, which are not
+// coherent with each other, 16 bytes a lane.
+template <int HD, int BM>
+struct Partials {
+  const PagedAttn &p;
+  int slots;
+
+  CRF_DEV float *o(int slot) const { return p.part + (int64_t)slot * BM * HD; }
+  CRF_DEV float2 *ml(int slot) const {
+    return (float2 *)(p.part + (int64_t)2 * slots * BM * HD) + (int64_t)slot * BM;
+  }
+  CRF_DEV void store(int slot, int at, f32x4 v) const {  // four floats from `at` on
+    constexpr int DEVICE = 16;  // cache policy: device scope
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), make_rsrc(o(slot), BM * HD * 4), at * 4, 0,
+                                           DEVICE);
+  }
+  CRF_DEV void store_ml(int slot, int r, float ref, float l) const {
+    __hip_atomic_store((uint64_t *)(ml(slot) + r),
+                       (uint64_t)__builtin_bit_cast(uint32_t, ref) | (uint64_t)__builtin_bit_cast(uint32_t, l) << 32,
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 };
 
-// Counts this workgroup's part of the unit as done; the one that finishes last
-// joins all parts.  ml: ML_CAP pairs of LDS that nobody uses.
-template <typename T, int HD, int BM, int NT>
-CRF_DEV void join(const Writer<T, HD> &wr, const Task &t, float2 *ml, int &last) {
-  const PagedAttn &p = wr.p;
-  const int tid = threadIdx.x;
+// Counts this workgroup's part of the unit as done; true for the one that finishes
+// last, which may then read all parts.
+CRF_DEV bool part_done(const PagedAttn &p, const Task &t, int &last) {
   agent_flush();
   __syncthreads();
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     last = agent_ticket(&p.tickets[t.owner]) == (unsigned)t.parts - 1;
-    if (last)
-      __hip_atomic_store(&p.tickets[t.owner], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (last) __hip_atomic_store(&p.tickets[t.owner], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if (!last) return;
+  if (!last) return false;
   // the others' parts are in memory: no line of them may be left in a cache
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  const int step = ML_CAP / t.parts;  // rows joined at a time
-  for (int r0 = 0; r0 < wr.rows; r0 += step) {
-    const int rows = min(step, wr.rows - r0);
-    for (int i = tid; i < rows * t.parts; i += NT) {
-      const int part = i % t.parts, r = r0 + i / t.parts;
-      ml[i] = *(const float2 *)(wr.template part_row<BM>(part_slot(t.owner, part), r) + HD);
-    }
-    __syncthreads();
-    for (int i = tid; i < rows * (HD / 4); i += NT) {
-      const int r = i / (HD / 4), e = 4 * (i % (HD / 4));
-      const float2 *m = ml + r * t.parts;
-      float ref = -INFINITY, l = 0.f;
-      for (int k = 0; k < t.parts; ++k) ref = fmaxf(ref, m[k].x);
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int k = 0; k < t.parts; ++k) {
-        // (a part of which the row sees nothing has no O)
-        const f32x4 x = *(const f32x4 *)(wr.template part_row<BM>(part_slot(t.owner, k), r0 + r) + e);
-        const bool some = m[k].y != 0.f;
-        const float w = some ? fast_exp2(m[k].x - ref) : 0.f;
-        l += w * m[k].y;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) o[v] = some ? fmaf(w, x[v], o[v]) : o[v];
-      }
-      const f32x4 one[1] = {o};
-      wr.out(r0 + r, e, one, ref, l);
-    }
-    __syncthreads();
-  }
+  return true;
 }
 
-CRF_DEV void st_ml(float *p, float ref, float l) {
-  __hip_atomic_store((uint64_t *)p,
-                     (uint64_t)__builtin_bit_cast(uint32_t, ref) | (uint64_t)__builtin_bit_cast(uint32_t, l) << 32,
-                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+// A row's running result over parts: U parts' references, sums and weights at a time.
+template <int U>
+struct Joined {
+  float ref = -INFINITY, l = 0.f, alpha, w[U];
+  // Parts k0 .. of row r: what the sum so far (alpha) and each part's O (w) weigh.  A part
+  // of which the row sees nothing weighs nothing.
+  template <typename P>
+  CRF_DEV void add(const P &parts, const Task &t, int k0, int r) {
+    float2 m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = parts.ml(part_slot(t.owner, min(k0 + u, t.parts - 1)))[r];
+    float top = ref;
+    bool some[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      some[u] = k0 + u < t.parts && m[u].y != 0.f;
+      if (some[u]) top = fmaxf(top, m[u].x);
+    }
+    alpha = l == 0.f ? 0.f : fast_exp2(ref - top);
+    l *= alpha;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      w[u] = some[u] ? fast_exp2(m[u].x - top) : 0.f;
+      l += w[u] * m[u].y;
+    }
+    ref = top;
+  }
+  CRF_DEV void plus(f32x4 &o, int u, f32x4 x) const {  // (an infinity of no weight stays out)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) o[v] = w[u] != 0.f ? fmaf(w[u], x[v], o[v]) : o[v];
+  }
+};
 
 // ---------------------------------------------------------------- keys and values from the pages
 
@@ -733,12 +766,12 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   __shared__ __align__(16) T ks0[TILE], ks1[TILE], vs0[TILE], vs1[TILE];
   __shared__ int pg[PGCAP];
   __shared__ int bad, last;
-  __shared__ ScheduleLds<NT> slds;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, p.g_div}, slots, may_many};
   const Shape &sh = sch.sh;
+  const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
   Task t;
 #pragma unroll 1
@@ -815,13 +848,37 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
       if (r < rows) wr.out(r, 4 * g, o, st.ref, l);
       continue;
     }
-    if (r < rows) {
-      float *dst = wr.template part_row<BM>(part_slot(t.owner, t.part), r);
+    // (partials in the order of the fragments: a load or store of a wave is 1 KiB in a row)
+    const int slot = part_slot(t.owner, t.part), mine = (wave * 4 * L::HB * 64 + lane) * 4;
 #pragma unroll
-      for (int i = 0; i < 4 * L::HB; ++i) st_agent16(dst + 8 * i + 4 * g, o[i]);
-      if (g == 0) st_ml(dst + HD, st.ref, l);
+    for (int i = 0; i < 4 * L::HB; ++i) parts.store(slot, mine + 256 * i, o[i]);
+    if (g == 0) parts.store_ml(slot, r, st.ref, l);
+    if (!part_done(p, t, last)) continue;
+#pragma unroll 1
+    for (int b = 0; b < L::HB; ++b) {
+      constexpr int U = 4;
+      Joined<U> j;
+      f32x4 sum[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int k = 0; k < t.parts; k += U) {
+        f32x4 x[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[u][i] = *(const f32x4 *)(parts.o(part_slot(t.owner, min(k + u, t.parts - 1))) + mine + 256 * (4 * b + i));
+        j.add(parts, t, k, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum[i] *= j.alpha;
+#pragma unroll
+          for (int u = 0; u < U; ++u) j.plus(sum[i], u, x[u][i]);
+        }
+      }
+      if (r < rows) wr.out(r, 32 * b + 4 * g, sum, j.ref, j.l);
     }
-    join<T, HD, BM, NT>(wr, t, (float2 *)vs0, last);
   }
 }
 
@@ -844,12 +901,12 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   __shared__ int pg[PGCAP];
   __shared__ float2 wml[NW][32];
   __shared__ int bad, last;
-  __shared__ ScheduleLds<NT> slds;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule<NT> sch{p, slds, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, p.g_div}, slots, may_many};
   const Shape &sh = sch.sh;
+  const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
   Task t;
 #pragma unroll 1
@@ -957,12 +1014,31 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         const f32x4 one[1] = {o};
         wr.out(r, 4 * c4, one, ref, l);
       } else {
-        float *dst = wr.template part_row<BM>(part_slot(t.owner, t.part), r);
-        st_agent16(dst + 4 * c4, o);
-        if (c4 == 0) st_ml(dst + HD, ref, l);
+        const int slot = part_slot(t.owner, t.part);
+        parts.store(slot, 4 * i, o);
+        if (c4 == 0) parts.store_ml(slot, r, ref, l);
       }
     }
-    if (t.parts > 1) join<T, HD, BM, NT>(wr, t, (float2 *)vs0, last);
+    if (t.parts == 1 || !part_done(p, t, last)) continue;
+#pragma unroll 1
+    for (int i = tid; i < rows * (HD / 4); i += NT) {
+      const int r = i / (HD / 4);
+      constexpr int U = 16;
+      Joined<U> j;
+      f32x4 o[1] = {{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 1
+      for (int k = 0; k < t.parts; k += U) {
+        f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          x[u] = *(const f32x4 *)(parts.o(part_slot(t.owner, min(k + u, t.parts - 1))) + 4 * i);
+        j.add(parts, t, k, r);
+        o[0] *= j.alpha;
+#pragma unroll
+        for (int u = 0; u < U; ++u) j.plus(o[0], u, x[u]);
+      }
+      wr.out(r, 4 * (i % (HD / 4)), o, j.ref, j.l);
+    }
   }
 }
 
@@ -975,13 +1051,14 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   p.least_keys = sizeof(T) == 2 ? 256 : 64;
   p.g_div = fast_div(G);
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
-  const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 4)) : 0;  // two slots a workgroup
+  const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 2)) : 0;  // two slots a workgroup
   int slots = (int)(room < resident ? room : resident);
   if (slots > PAGED_TICKETS) slots = PAGED_TICKETS;
   slots = slots / 8 * 8;
   // (a sequence's last tile may be short)
   const int64_t most = ((int64_t)p.b.n_rows * G / bm + p.b.n_seqs) * p.nkv;
-  const bool may_many = most >= (int64_t)MANY * slots;
+  // (units of single tokens are all alike: stretches of them balance as well)
+  const bool may_many = slots == 0 || (!keys && most >= (int64_t)MANY * slots);
   const int64_t grid = may_many ? most : slots;
   if (grid < 1) return hipSuccess;
   const dim3 g((unsigned)(grid < (1 << 24) ? grid : 1 << 24));

@@ -26,7 +26,7 @@ int main() {
   for (int it = 0; it < 4000; ++it) {
     const int nkv = 1 + upto(7), G = 1 + upto(8), bm = it % 2 ? 32 : 128;
     const int window = upto(3) ? 0 : 1 + upto(3000);
-    const Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, fast_div(G)};
+    const Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), fast_div(G)};
     const int slots = 8 * (1 + upto(63)), seqs = 1 + upto(40);
     const int most_new = bm == 32 ? (32 / G > 0 ? 32 / G : 1) : 1 + upto(1 + upto(2000));
     std::vector<int> n(seqs), len(seqs);
@@ -67,7 +67,7 @@ int main() {
     // dealt out
     double share;
     int n_wg;
-    deal(total, 256.0 * G, slots, share, n_wg);
+    deal(total, 256.0 * G, seqs * nkv, slots, share, n_wg);
     if (n_wg < 1 || n_wg > slots) return fail("more workgroups than slots", it);
     std::set<int> stretches;
     for (int b = 0; b < slots; ++b) {
