@@ -231,8 +231,9 @@ def kv_cache(k_pool, v_pool, block_table, n_tokens: int, page_size: int) -> KVCa
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        # (the pointer itself: a torch.cuda.Stream object around it takes 3 us to make)
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
@@ -399,21 +400,21 @@ def _same_device(*tensors) -> int:
     return dev
 
 
-def _check_device(ctx: Context, *parts):
-    """Tensors and descriptors of a call lie on the context's device."""
-    for t in parts:
-        if t is None:
-            continue
-        dev = t.device if isinstance(t, ctypes.Structure) else t.get_device()
-        if dev != ctx.device:
-            raise CrfError(1, f"a tensor on {'the host' if dev < 0 else f'device {dev}'}, the context on device {ctx.device}")
+def _check_device(ctx: Context, descriptors, tensors):
+    """Descriptors and tensors of a call lie on the context's device."""
+    dev = ctx.device
+    for d in descriptors:
+        if d.device != dev:
+            raise CrfError(1, f"tensors {'on the host' if d.device < 0 else f'of device {d.device}'}, context of device {dev}")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise CrfError(1, f"a tensor {'on the host' if not t.is_cuda else f'of {t.device}'}, context of device {dev}")
 
 
 def _int32(t, n: Optional[int], name: str):
     """A contiguous int32 device vector (of n values)."""
     import torch
-    if t.dtype is not torch.int32 or t.dim() != 1 or (t.numel() > 1 and t.stride(0) != 1) or \
-            (n is not None and t.numel() != n):
+    if t.dtype is not torch.int32 or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
         raise CrfError(2, f"{name} must be a contiguous int32 vector" + (f" of {n}" if n is not None else ""))
     return t
 
@@ -425,23 +426,24 @@ def _tables(t):
     return t
 
 
-def _head_rows(ctx: Context, t, n_rows: int, heads: int, name: str):
-    """Pointer and row stride of [rows, heads, head_dim] or [rows, heads * head_dim] whose rows are contiguous."""
+def _storage(dims: ModelDims):
+    """The torch type of the context's storage type."""
     import torch
-    d = ctx.dims
-    want = torch.bfloat16 if d.dtype == CRF_BF16 else torch.float32
-    if t.dtype is not want:
-        raise CrfError(1, f"{name} is {t.dtype}, the context's storage type {want}")
-    shape, stride = t.shape, t.stride()
-    ok = shape[0] == n_rows and stride[-1] == 1
+    return torch.bfloat16 if dims.dtype == CRF_BF16 else torch.float32
+
+
+def _head_rows(d: ModelDims, t, n_rows: int, heads: int, name: str):
+    """Pointer and row stride of [rows, heads, head_dim] or [rows, heads * head_dim] whose rows are contiguous."""
+    shape, stride, hd = t.shape, t.stride(), d.head_dim
+    if t.dtype is not _storage(d):
+        raise CrfError(1, f"{name} is {t.dtype}, the context's storage type differs")
     if len(shape) == 3:
-        ok = ok and shape[1] == heads and shape[2] == d.head_dim and (heads == 1 or stride[1] == d.head_dim)
+        ok = shape[1] == heads and shape[2] == hd and (heads == 1 or stride[1] == hd)
     else:
-        ok = ok and len(shape) == 2 and shape[1] == heads * d.head_dim
-    if not ok:
-        raise CrfError(2, f"{name} {tuple(shape)} (strides {stride}) is not {n_rows} rows of {heads} heads of "
-                          f"{d.head_dim}")
-    return t.data_ptr(), stride[0] if n_rows > 1 else heads * d.head_dim
+        ok = len(shape) == 2 and shape[1] == heads * hd
+    if not ok or shape[0] != n_rows or stride[-1] != 1:
+        raise CrfError(2, f"{name} {tuple(shape)} (strides {stride}) is not {n_rows} rows of {heads} heads of {hd}")
+    return t.data_ptr(), stride[0] if n_rows > 1 else heads * hd
 
 
 def page_pool(k_pool, v_pool, page_size: int) -> PagePool:
@@ -451,19 +453,18 @@ def page_pool(k_pool, v_pool, page_size: int) -> PagePool:
         raise CrfError(2, "pools must be two like tensors [layers, pages, kv heads, page_size, head_dim], pages contiguous")
     p = PagePool(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), k_pool.stride(1), k_pool.shape[1], page_size)
     p.tensors, p.device = (k_pool, v_pool), _same_device(k_pool, v_pool)
+    p.layers, p.heads, p.head_dim = k_pool.shape[0], k_pool.shape[2], k_pool.shape[4]
     return p
 
 
-def _check_pool(ctx: Context, pool: PagePool, layers: int):
+def _check_pool(d: ModelDims, pool: PagePool, layers: int):
     """The pool's storage type and heads are the context's, and it has that many layers."""
-    import torch
-    k, d = pool.tensors[0], ctx.dims
-    if k.dtype is not (torch.bfloat16 if d.dtype == CRF_BF16 else torch.float32):
-        raise CrfError(1, f"the pool is {k.dtype}, the context's storage type differs")
-    if k.shape[2] != d.n_kv_heads or k.shape[4] != d.head_dim:
-        raise CrfError(2, f"the pool has {k.shape[2]} heads of {k.shape[4]}, the context {d.n_kv_heads} of {d.head_dim}")
-    if not 0 <= layers <= k.shape[0]:
-        raise CrfError(3, f"{layers} layers of a pool of {k.shape[0]}")
+    if pool.tensors[0].dtype is not _storage(d):
+        raise CrfError(1, f"the pool is {pool.tensors[0].dtype}, the context's storage type differs")
+    if pool.heads != d.n_kv_heads or pool.head_dim != d.head_dim:
+        raise CrfError(2, f"the pool has {pool.heads} heads of {pool.head_dim}, the context {d.n_kv_heads} of {d.head_dim}")
+    if not 0 <= layers <= pool.layers:
+        raise CrfError(3, f"{layers} layers of a pool of {pool.layers}")
 
 
 def seq_batch(row_start, length, block_tables, n_rows: int, max_new: int = 0) -> SeqBatch:
@@ -493,13 +494,13 @@ def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePo
                 positions=None, stream=None):
     """crf_rope_append: q rotated into q_out (both None: keys and values only), k rotated and v into the pages."""
     d, n = ctx.dims, batch.n_rows
-    _check_pool(ctx, pool, layer + 1)
-    qp, qs = _head_rows(ctx, q, n, d.n_q_heads, "q") if q is not None else (None, 0)
-    op, os_ = _head_rows(ctx, q_out, n, d.n_q_heads, "q_out") if q_out is not None else (None, 0)
-    kp, ks = _head_rows(ctx, k, n, d.n_kv_heads, "k")
-    vp, vs = _head_rows(ctx, v, n, d.n_kv_heads, "v")
+    _check_pool(ctx.dims, pool, layer + 1)
+    qp, qs = _head_rows(d, q, n, d.n_q_heads, "q") if q is not None else (None, 0)
+    op, os_ = _head_rows(d, q_out, n, d.n_q_heads, "q_out") if q_out is not None else (None, 0)
+    kp, ks = _head_rows(d, k, n, d.n_kv_heads, "k")
+    vp, vs = _head_rows(d, v, n, d.n_kv_heads, "v")
     pp = _int32(positions, n, "positions").data_ptr() if positions is not None else None
-    _check_device(ctx, batch, pool, q, k, v, q_out, positions)
+    _check_device(ctx, (batch, pool), (q, k, v, q_out, positions))
     st = ctx.lib.crf_rope_append(ctx.handle, rope, batch, pp, qp, qs, kp, ks, vp, vs, op, os_, pool, layer,
                                  _stream(stream))
     _err(ctx.lib, ctx.handle, st)
@@ -509,14 +510,13 @@ def paged_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int
                     window: int = 0, stream=None):
     """crf_paged_attention: out [rows, heads, head_dim] (and lse, fp32 [rows, heads]) of the new tokens' queries q."""
     d, n = ctx.dims, batch.n_rows
-    _check_pool(ctx, pool, layer + 1)
-    qp, qs = _head_rows(ctx, q, n, d.n_q_heads, "q")
-    op, os_ = _head_rows(ctx, out, n, d.n_q_heads, "out")
+    _check_pool(ctx.dims, pool, layer + 1)
+    qp, qs = _head_rows(d, q, n, d.n_q_heads, "q")
+    op, os_ = _head_rows(d, out, n, d.n_q_heads, "out")
     if lse is not None:
-        import torch
-        if lse.dtype is not torch.float32 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
+        if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
             raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
-    _check_device(ctx, batch, pool, q, out, lse)
+    _check_device(ctx, (batch, pool), (q, out, lse))
     st = ctx.lib.crf_paged_attention(ctx.handle, batch, qp, qs, pool, layer, scale, window, op, os_, _ptr(lse),
                                      _stream(stream))
     _err(ctx.lib, ctx.handle, st)
@@ -527,11 +527,11 @@ def pages_copy(ctx: Context, pool: PagePool, src, dst, l0: int = 0, h: Optional[
     """crf_pages_copy: pages src of `pool` to pages dst of `to` (None: the same pool), layers [l0, l0 + h)."""
     h = pool.tensors[0].shape[0] - l0 if h is None else h
     to, to_l0 = pool if to is None else to, l0 if to_l0 is None else to_l0
-    _check_pool(ctx, pool, l0 + h)
-    _check_pool(ctx, to, to_l0 + h)
+    _check_pool(ctx.dims, pool, l0 + h)
+    _check_pool(ctx.dims, to, to_l0 + h)
     n = src.numel()
     sp, dp = _int32(src, n, "src").data_ptr(), _int32(dst, n, "dst").data_ptr()
-    _check_device(ctx, pool, to, src, dst)
+    _check_device(ctx, (pool, to), (src, dst))
     st = ctx.lib.crf_pages_copy(ctx.handle, pool, l0, to, to_l0, h, n, sp, dp, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
@@ -548,10 +548,10 @@ def page_map(refs, block_tables, lengths, page_size: int) -> PageMap:
 
 def pages_fork(ctx: Context, pool: PagePool, map: PageMap, parents, children, stream=None):
     """crf_pages_fork: children[i] becomes a copy of parents[i] that shares its full pages."""
-    _check_pool(ctx, pool, ctx.dims.n_layers)
+    _check_pool(ctx.dims, pool, ctx.dims.n_layers)
     n = parents.numel()
     pp, cp = _int32(parents, n, "parents").data_ptr(), _int32(children, n, "children").data_ptr()
-    _check_device(ctx, pool, map, parents, children)
+    _check_device(ctx, (pool, map), (parents, children))
     st = ctx.lib.crf_pages_fork(ctx.handle, pool, map, n, pp, cp, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
@@ -559,7 +559,7 @@ def pages_fork(ctx: Context, pool: PagePool, map: PageMap, parents, children, st
 def pages_extend(ctx: Context, map: PageMap, n_new, stream=None):
     """crf_pages_extend: every sequence s grows by n_new[s] tokens."""
     gp = _int32(n_new, map.n_seqs, "n_new").data_ptr()
-    _check_device(ctx, map, n_new)
+    _check_device(ctx, (map,), (n_new,))
     st = ctx.lib.crf_pages_extend(ctx.handle, map, gp, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
@@ -568,15 +568,15 @@ def pages_free(ctx: Context, map: PageMap, seqs, stream=None):
     """crf_pages_free: the sequences end."""
     n = seqs.numel()
     sp = _int32(seqs, n, "seqs").data_ptr()
-    _check_device(ctx, map, seqs)
+    _check_device(ctx, (map,), (seqs,))
     st = ctx.lib.crf_pages_free(ctx.handle, map, n, sp, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 
 def pages_compact(ctx: Context, pool: PagePool, map: PageMap, map_out: PageMap, remap, counts, stream=None):
     """crf_pages_compact: the pages in use move to the front of the pool; map_out may be map."""
-    _check_pool(ctx, pool, ctx.dims.n_layers)
+    _check_pool(ctx.dims, pool, ctx.dims.n_layers)
     rp, cp = _int32(remap, map.n_pages, "remap").data_ptr(), _int32(counts, 2, "counts").data_ptr()
-    _check_device(ctx, pool, map, map_out, remap, counts)
+    _check_device(ctx, (pool, map, map_out), (remap, counts))
     st = ctx.lib.crf_pages_compact(ctx.handle, pool, map, map_out, rp, cp, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
