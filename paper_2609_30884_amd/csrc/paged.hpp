@@ -89,8 +89,10 @@ struct PagedAttn {
   unsigned *tickets;   // PAGED_TICKETS, zero between launches
   const char *zeros;   // PAGED_ZERO_BYTES
   int n_cu;
-  int least_keys;      // keys that are worth a workgroup (set by the launcher, as g_div)
+  // set by the launcher
   FastDiv g_div;       // by nq / nkv
+  double spread;       // workgroups wanted: work x spread, or its root
+  bool spread_root;
 };
 hipError_t launch_paged_attn(hipStream_t s, bool f32, const PagedAttn &p);
 

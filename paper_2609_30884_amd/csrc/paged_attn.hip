@@ -49,14 +49,40 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 CRF_DEV float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-CRF_DEV s16x4 ld_tr(const bf16 *p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(const __attribute__((address_space(3))) void *)p);
-}
 CRF_DEV f32x16 mfma32f(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-// 16 bytes a lane from global memory to lds + 16 * lane
-CRF_DEV void gload16(const char *g, void *lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
-                                   (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+typedef __attribute__((address_space(3))) char lds_mem;
+CRF_DEV u32x4 lds16(const lds_mem *p) { return *(const __attribute__((address_space(3))) u32x4 *)p; }
+CRF_DEV s16x4 lds_tr(const lds_mem *p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p); }
+
+// Loads of 16 bytes a lane straight to LDS, lane L's to lds + 16 L, for K and V
+// together.  Written out, so that the compiler neither waits for them by itself (it would
+// before every read of an LDS address that it cannot tell apart) nor needs a copy of the
+// loop for each stage: they have no register to return to, and the kernels wait by count
+// before they read.  M0, which nothing else here uses, takes the LDS address; the first
+// wait states are those between a lane read into a scalar register and a vector memory
+// instruction that uses it, the others those between M0 and its use.
+//
+// One page: raw buffer resources of the K and V rows (loads past their end return zero).
+CRF_DEV u32x4 resource(const void *base, uint32_t bytes) {
+  const uint64_t a = (uint64_t)base;
+  return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+CRF_DEV void dma_page(u32x4 kr, u32x4 vr, const lds_mem *kl, const lds_mem *vl, uint32_t ko, uint32_t vo) {
+  asm volatile(
+      "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds"
+      :
+      : "s"(kl), "s"(vl), "v"(ko), "v"(vo), "s"(kr), "s"(vr)
+      : "memory");
+}
+// Rows of their own: an address a lane.
+CRF_DEV void dma_row(const char *k, const char *v, const lds_mem *kl, const lds_mem *vl) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off"
+      :
+      : "s"(kl), "s"(vl), "v"(k), "v"(v)
+      : "memory");
 }
 
 template <typename T, int HD>
@@ -135,11 +161,11 @@ struct RowState {
   }
 };
 
-// Raw scores of NB blocks of 32 keys (LDS rows r0 ..) against the wave's 32 rows.
+// Raw scores of NB blocks of 32 keys (K rows from kt on) against the wave's 32 rows.
 // bf16: the K fragments are read two steps ahead of the products that use them (the
 // scheduling barriers keep the compiler from regrouping them).
 template <typename T, int HD, int NB>
-CRF_DEV void scores(const T *kt, int r0, const QFrag<T, HD> &q, int lane, f32x16 (&s)[NB]) {
+CRF_DEV void scores(const lds_mem *kt, const QFrag<T, HD> &q, int lane, f32x16 (&s)[NB]) {
   using L = Layout<T, HD>;
   f32x16 zero;
 #pragma unroll
@@ -149,7 +175,7 @@ CRF_DEV void scores(const T *kt, int r0, const QFrag<T, HD> &q, int lane, f32x16
   fresh(ka);
   auto kread = [&](int step, u32x4 (&f)[NB]) {
 #pragma unroll
-    for (int kb = 0; kb < NB; ++kb) f[kb] = ld16((const char *)kt + (r0 + 32 * kb) * L::ROWB + (ka ^ (32 * step)));
+    for (int kb = 0; kb < NB; ++kb) f[kb] = lds16(kt + 32 * kb * L::ROWB + (ka ^ (32 * step)));
   };
   kread(0, kf[0]);
   kread(1, kf[1]);
@@ -171,16 +197,16 @@ CRF_DEV void scores(const T *kt, int r0, const QFrag<T, HD> &q, int lane, f32x16
   }
 }
 
-// How a block of keys is taken.  ALL: every row sees all of it.  SOME: some row does
-// not see some key.  CAREFUL: the same where a value that is not finite may belong to
+// How a block of keys is taken.  ALL: every row sees all of it and keeps its reference.
+// SOME: some row does not see some key, or needs another reference.  CAREFUL: the same where a value that is not finite may belong to
 // a key that some row does not see: the product would multiply it by that row's
 // weight zero, so such values are taken out of the product and added where the weight
 // is not zero.  (Units run with SOME first, and again if their result is not finite.)
 enum Take { ALL, SOME, CAREFUL };
 
-// O += P V for the probabilities p of 32 keys in LDS rows r0 ...
+// O += P V for the probabilities p of 32 keys (V rows from vt on).
 template <typename T, int HD, Take TAKE>
-CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, int lane) {
+CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, int lane) {
   using L = Layout<T, HD>;
   uint32_t va = L::vaddr(lane);
   fresh(va);
@@ -210,7 +236,7 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          x[h][k] = ld_tr((const bf16 *)((const char *)vt + (r0 + 16 * h + 8 * k) * L::ROWB + (va ^ (64 * b))));
+          x[h][k] = lds_tr(vt + (16 * h + 8 * k) * L::ROWB + (va ^ (64 * b)));
       if constexpr (TAKE == CAREFUL) {
         f32x16 zero;
 #pragma unroll
@@ -242,7 +268,7 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
       float x[16];
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        x[v] = *(const float *)((const char *)vt + (r0 + 8 * (v / 4) + v % 4) * L::ROWB + 128 * b + va);
+        x[v] = *(const __attribute__((address_space(3))) float *)(vt + (8 * (v / 4) + v % 4) * L::ROWB + 128 * b + va);
       if constexpr (TAKE == CAREFUL) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
@@ -261,63 +287,88 @@ CRF_DEV void weigh(const T *vt, int r0, const float (&p)[16], RowState<HD> &st, 
   }
 }
 
-// NB blocks of 32 keys, key0 .. in LDS rows r0 ..: scores, probabilities, O += P V.
-template <typename T, int HD, Take TAKE, int NB>
-CRF_DEV void blocks(const T *kt, const T *vt, int r0, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
-                    int lane, const Seen &seen) {
-  const int g = lane / 32;
+// NB blocks of 32 keys that every row sees.  False, with nothing
+// changed, if some row needs another reference: then the blocks are taken one by one
+// as below (the code that rescales O stays out of the loop over the others).
+template <typename T, int HD, int NB>
+CRF_DEV bool whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, HD> &q, RowState<HD> &st, float c,
+                          int lane) {
   f32x16 s[NB];
-  scores<T, HD, NB>(kt, r0, q, lane, s);
+  scores<T, HD, NB>(kt, q, lane, s);
+  float p[NB][16], sum[NB];
+  bool raise = false;
 #pragma unroll
   for (int kb = 0; kb < NB; ++kb) {
-    if constexpr (TAKE != ALL) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int key = key0 + 32 * kb + 8 * (v / 4) + 4 * g + v % 4;
-        if (key < seen.lo || key > seen.hi) s[kb][v] = -INFINITY;
-      }
-      if (seen.bad) {
-#pragma unroll 1
-        for (int i = 0; i < 32; ++i) {  // keys of pages out of range
-          const int key = key0 + 32 * kb + i;
-          if (key < seen.end && seen.pages[div_by(key, seen.ps_div) - seen.first] < 0)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-              if (8 * (v / 4) + 4 * g + v % 4 == i) s[kb][v] = -INFINITY;
-        }
-      }
-    }
-    float p[16], sum = 0.f;
+    sum[kb] = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      p[v] = fast_exp2(fmaf(s[kb][v], c, -st.ref));
+      p[kb][v] = fast_exp2(fmaf(s[kb][v], c, -st.ref));
+      sum[kb] += p[kb][v];
+    }
+    raise |= !(sum[kb] <= PSUM_MAX);  // (also where the sum is no number)
+  }
+  if (__builtin_amdgcn_ballot_w64(raise)) return false;
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb) {
+    st.l += sum[kb];
+    weigh<T, HD, ALL>(vt + 32 * kb * Layout<T, HD>::ROWB, p[kb], st, lane);
+  }
+  return true;
+}
+
+// One block of 32 keys, key0 ..: scores, probabilities, O += P V.
+template <typename T, int HD, Take TAKE>
+CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
+                   int lane, const Seen &seen) {
+  const int g = lane / 32;
+  f32x16 sc[1];
+  scores<T, HD, 1>(kt, q, lane, sc);
+  f32x16 &s = sc[0];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    const int key = key0 + 8 * (v / 4) + 4 * g + v % 4;
+    if (key < seen.lo || key > seen.hi) s[v] = -INFINITY;
+  }
+  if (seen.bad) {
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i) {  // keys of pages out of range
+      const int key = key0 + i;
+      if (key < seen.end && seen.pages[div_by(key, seen.ps_div) - seen.first] < 0)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (8 * (v / 4) + 4 * g + v % 4 == i) s[v] = -INFINITY;
+    }
+  }
+  float p[16], sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    p[v] = fast_exp2(fmaf(s[v], c, -st.ref));
+    sum += p[v];
+  }
+  if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+    // only rows that need one: a row's result does not depend on the tile's others
+    const float other = __shfl_xor(sum, 32, 64);
+    const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
+    const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
+    const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
+    const float base = ref == -INFINITY ? 0.f : ref;  // (a row that has seen no key yet)
+    st.ref = ref;
+    st.l *= alpha;
+#pragma unroll
+    for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
+    sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      p[v] = fast_exp2(fmaf(s[v], c, -base));
       sum += p[v];
     }
-    if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {  // (also where the sum is no number)
-      float mx = -INFINITY;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
-      // only rows that need one: a row's result does not depend on the tile's others
-      const float other = __shfl_xor(sum, 32, 64);
-      const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
-      const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
-      const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
-      const float base = ref == -INFINITY ? 0.f : ref;
-      st.ref = ref;
-      st.l *= alpha;
-#pragma unroll
-      for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
-      sum = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        p[v] = fast_exp2(fmaf(s[kb][v], c, -base));
-        sum += p[v];
-      }
-    }
-    st.l += sum;
-    weigh<T, HD, TAKE>(vt, r0 + 32 * kb, p, st, lane);
   }
+  st.l += sum;
+  weigh<T, HD, TAKE>(vt, p, st, lane);
 }
 
 // ---------------------------------------------------------------- schedule
@@ -337,11 +388,16 @@ struct SeqWork {
   }
 };
 
-// floor(a / b) for whole a >= 0, b > 0
+// floor(a / b) for whole a >= 0, b > 0: by a reciprocal in 32 bits, put right (a
+// division in 64 bits costs three times the instructions)
 __host__ __device__ inline double quotient(double a, double b) {
+#ifdef __HIP_DEVICE_COMPILE__
+  double q = floor(a * (double)__builtin_amdgcn_rcpf((float)b));
+#else
   double q = floor(a / b);
-  if (q * b > a) q -= 1;
-  if (a - q * b >= b) q += 1;
+#endif
+  while (q * b > a) q -= 1;
+  while (a - q * b >= b) q += 1;
   return q;
 }
 
@@ -357,6 +413,7 @@ struct Task {
 struct Shape {
   int G, nkv, window, bm, bkv;  // query heads of a KV head; rows and keys of a tile
   int over;                     // keys that a unit costs besides its own
+  double pad;                   // and work added by the dealing
   FastDiv g_div;                // by G
 
   __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
@@ -372,7 +429,7 @@ struct Shape {
       const double room = w.cap - w.base;
       if (room < (double)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
     }
-    w.over = (double)over * G;
+    w.over = (double)over * G + pad;
     return w;
   }
   // All of a sequence's work, or (units) its units.
@@ -427,15 +484,34 @@ struct Shape {
   }
 };
 
-// Work of a workgroup when `total` is dealt out to at most `slots`, and how many get
-// any: no fewer than `heads` (the sequences' KV heads, which need not wait for each
-// other) and as many as have `least` each.
-__host__ __device__ inline void deal(double total, double least, int heads, int slots, double &share, int &n_wg) {
-  double want = quotient(total, least);
-  want = want < heads ? heads : want;
+// How `total` work is dealt out to `n_wg` workgroups, `share` each: `want` of them, but
+// no fewer than there are heads (the sequences' KV heads, which need not wait for each
+// other) and no more than `slots`.  one > 0: every head has that much, as
+// a single tile; then no border lies inside a head that a neighbour's stretch reaches
+// into: heads are padded to whole stretches, or a stretch holds whole heads.
+struct Deal {
+  double share, pad;  // pad: work added to every unit
+  int n_wg;
+};
+__host__ __device__ inline Deal deal(double total, double want, int heads, double one, int slots) {
+  Deal d;
+  want = floor(want < heads ? heads : want);
   want = want < slots ? want : slots;
-  share = quotient(total + want - 1, want);
-  n_wg = (int)quotient(total + share - 1, share);
+  d.pad = 0;
+  if (one > 0 && want >= heads) {
+    const double parts = quotient(want, heads);
+    d.share = quotient(one + parts - 1, parts);
+    d.pad = d.share * parts - one;
+    d.n_wg = heads * (int)parts;
+  } else if (one > 0) {
+    const double per = quotient(heads + want - 1, want);
+    d.share = one * per;
+    d.n_wg = (int)quotient(heads + per - 1, per);
+  } else {
+    d.share = quotient(total + want - 1, want);
+    d.n_wg = (int)want;  // (the last ones' stretches may begin past the end)
+  }
+  return d;
 }
 
 // Stretch of workgroup `bid`: neighbouring stretches, which share keys, lie on one
@@ -528,17 +604,34 @@ struct Schedule {
         end = total;
       } else {
         if (__builtin_amdgcn_readfirstlane(total == 0)) return false;
-        int n_wg;
-        deal(total, (double)p.least_keys * sh.G, p.b.n_seqs * sh.nkv, slots, share, n_wg);
-        share = lane_value(share, 0);
-        wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(n_wg));
+        // sequences of one tile and one length?
+        double one = 0;
+        int heads = p.b.n_seqs * sh.nkv;
+        const uint64_t active = __builtin_amdgcn_ballot_w64(q.v > 0);
+        if (p.b.n_seqs <= 64) {
+          const double v = lane_value(q.v, __builtin_ctzll(active));
+          heads = __popcll(active) * sh.nkv;
+          if (!__builtin_amdgcn_ballot_w64(q.v > 0 && (q.v != v || q.n * sh.G > sh.bm))) one = v / sh.nkv;
+        }
+        const double want = p.spread_root ? (double)sqrtf((float)(total * p.spread)) : total * p.spread;
+        const Deal d = deal(total, want, heads, one, slots);
+        share = lane_value(d.share, 0);
+        sh.pad = lane_value(d.pad, 0);
+        wg = stretch_of(blockIdx.x, __builtin_amdgcn_readfirstlane(d.n_wg));
         if (wg < 0) return false;
+        total += sh.pad * heads;
         at = wg * share;
         end = at + share < total ? at + share : total;
-        if (p.b.n_seqs <= 64)  // the pass has seen them all
+        if (__builtin_amdgcn_readfirstlane(at >= end)) return false;
+        if (p.b.n_seqs <= 64) {  // the pass has seen them all
+          if (q.v > 0) {
+            q.from += sh.pad * sh.nkv * __popcll(active & (((uint64_t)1 << (threadIdx.x % 64)) - 1));
+            q.v += sh.pad * sh.nkv;
+          }
           hold(at, q);
-        else
+        } else {
           pass(at, false, q);
+        }
       }
     }
     if (__builtin_amdgcn_readfirstlane(at >= end)) return false;
@@ -714,7 +807,7 @@ struct Pages {
   }
 
   // Keys key0 .. (a multiple of ROWS): always 2 * ROWS / RPI loads.
-  CRF_DEV void load(int key0, T *kdst, T *vdst) const {
+  CRF_DEV void load(int key0, const lds_mem *kdst, const lds_mem *vdst) const {
     const int lrow = lane / L::CH;
     uint32_t k0 = lrow * L::ROWB + L::kslot(lds_row0 + lrow, lane % L::CH) * 16;
     uint32_t v0 = lrow * L::ROWB + L::vslot(lrow, lane % L::CH) * 16;
@@ -723,19 +816,17 @@ struct Pages {
 #pragma unroll
     for (int g0 = 0; g0 < ROWS; g0 += GRP) {
       const int kg = key0 + g0;
-      char *kl = (char *)kdst + (lds_row0 + g0) * L::ROWB, *vl = (char *)vdst + (lds_row0 + g0) * L::ROWB;
+      const lds_mem *kl = kdst + (lds_row0 + g0) * L::ROWB, *vl = vdst + (lds_row0 + g0) * L::ROWB;
       if constexpr (UNI) {
         const int lp = div_by(kg, b.ps_div), rows = min(len - kg, GRP);
         const int q = rows > 0 ? __builtin_amdgcn_readfirstlane(pg[lp - first]) : -1;
         const int64_t off =
             q < 0 ? 0 : q * b.page_bytes + (int64_t)(kvh * b.page_size + kg - lp * b.page_size) * L::ROWB;
         const uint32_t bytes = q < 0 ? 0 : rows * L::ROWB;
-        const __amdgpu_buffer_rsrc_t kr = make_rsrc(b.k + off, bytes), vr = make_rsrc(b.v + off, bytes);
+        const u32x4 kr = resource(b.k + off, bytes), vr = resource(b.v + off, bytes);
 #pragma unroll
-        for (int i = 0; i < GRP / L::RPI; ++i) {
-          dma16(kr, (lds_char *)(kl + i * 1024), kbytes(i, k0) + i * 1024, 0);
-          dma16(vr, (lds_char *)(vl + i * 1024), v0 + i * 1024, 0);
-        }
+        for (int i = 0; i < GRP / L::RPI; ++i)
+          dma_page(kr, vr, kl + i * 1024, vl + i * 1024, kbytes(i, k0) + i * 1024, v0 + i * 1024);
       } else {
 #pragma unroll
         for (int i = 0; i < GRP / L::RPI; ++i) {
@@ -747,8 +838,7 @@ struct Pages {
             slot = key - lp * b.page_size;
           }
           const int64_t o = q * b.page_bytes + (int64_t)(kvh * b.page_size + slot - lrow) * L::ROWB;
-          gload16(q >= 0 ? b.k + o + kbytes(i, k0) : zeros, kl + i * 1024);
-          gload16(q >= 0 ? b.v + o + v0 : zeros, vl + i * 1024);
+          dma_row(q >= 0 ? b.k + o + kbytes(i, k0) : zeros, q >= 0 ? b.v + o + v0 : zeros, kl + i * 1024, vl + i * 1024);
         }
       }
     }
@@ -760,16 +850,14 @@ struct Pages {
 template <typename T, int HD, bool UNI>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots, bool may_many) {
   using L = Layout<T, HD>;
-  constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW, BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * HD;
-  // one array per stage and operand, so that the compiler sees that loads into one
-  // stage do not touch the other
-  __shared__ __align__(16) T ks0[TILE], ks1[TILE], vs0[TILE], vs1[TILE];
+  constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW, BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * L::ROWB;
+  __shared__ __align__(16) char stages[2][2 * TILE];  // K, then V
   __shared__ int pg[PGCAP];
   __shared__ int bad, last;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div}, slots, may_many};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
@@ -790,6 +878,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
     Pages<T, HD, UNI, BKV / NW> pages{p.b, p.zeros, pg, &bad, 0, t.len, t.kvh, wave * (BKV / NW), lane,
                                       p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
+    const int whole_to = wave * 32 < rows ? pos_lo + 1 : 0;  // keys before it are seen by every row of the wave
     const int end_key = t.t1 * BKV;
     if (tid == 0) bad = 0;
     bool careful = false;
@@ -797,42 +886,54 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
     for (;;) {
       st.clear();
       __syncthreads();  // the task (or the pass) before has left LDS
+      const lds_mem *mem = (const lds_mem *)&stages[0][0];
+      auto load = [&](int it, int stage) {
+        const lds_mem *k = mem + stage * 2 * TILE;
+        pages.load(it * BKV + wave * (BKV / NW), k, k + TILE);
+      };
       if (t.t0 < t.t1) {
         pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
         __syncthreads();
-        pages.load(t.t0 * BKV + wave * (BKV / NW), ks0, vs0);
+        load(t.t0, 0);
       }
-#pragma unroll 1
-      for (int it = t.t0; it < t.t1; ++it) {
-        const int kt0 = it * BKV;
-        const bool second = (it - t.t0) & 1;
+      // A tile's data is there, the next one's is on its way (each wave passes here once a
+      // tile, wherever it then goes).
+      auto arrive = [&](int it) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (it + 1 < t.t1) {
-          if (div_by(min(kt0 + 2 * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
-            pages.fill(div_by(kt0, p.b.ps_div), end_key, NT);
+          if (div_by(min((it + 2) * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
+            pages.fill(div_by(it * BKV, p.b.ps_div), end_key, NT);
             __syncthreads();
           }
-          if (second)
-            pages.load(kt0 + BKV + wave * (BKV / NW), ks0, vs0);
-          else
-            pages.load(kt0 + BKV + wave * (BKV / NW), ks1, vs1);
+          load(it + 1, (it + 1 - t.t0) & 1);
         }
-        if (wave * 32 >= rows || kt0 > pos_hi || kt0 + BKV <= first_seen) continue;
-        const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, pages.first, p.b.ps_div};
-        if (kt0 + BKV - 1 > pos_lo || kt0 < last_first || seen.bad) {
-          const T *kt = second ? ks1 : ks0, *vt = second ? vs1 : vs0;
+      };
+#pragma unroll 1
+      for (int it = t.t0; it < t.t1;) {
+        // tiles that every row of the wave sees; the first block of all gives the rows
+        // their reference
+        for (;;) {
+          arrive(it);
+          const int kt0 = it * BKV;
+          if (it == t.t0 || kt0 + BKV > whole_to || kt0 < last_first || bad) break;
+          const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
+          if (!whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
+          if (++it == t.t1) break;
+        }
+        if (it == t.t1) break;
+        const int kt0 = it * BKV;
+        if (wave * 32 < rows && kt0 <= pos_hi && kt0 + BKV > first_seen) {
+          const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, pages.first, p.b.ps_div};
+          const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
 #pragma unroll 1
           for (int kb = 0; kb < BKV; kb += 32)
             if (careful)
-              blocks<T, HD, CAREFUL, 1>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
+              block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane, seen);
             else
-              blocks<T, HD, SOME, 1>(kt, vt, kb, kt0 + kb, q, st, p.scale_log2, lane, seen);
-        } else if (second) {
-          blocks<T, HD, ALL, BKV / 32>(ks1, vs1, 0, kt0, q, st, p.scale_log2, lane, seen);
-        } else {
-          blocks<T, HD, ALL, BKV / 32>(ks0, vs0, 0, kt0, q, st, p.scale_log2, lane, seen);
+              block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane, seen);
         }
+        ++it;
       }
       if (careful || !__syncthreads_or(!st.finite())) break;
       careful = true;
@@ -895,16 +996,16 @@ template <typename T, int HD, bool UNI>
 __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_CU)) void attn_keys_kernel(
     const PagedAttn p, int slots, bool may_many) {
   using L = Layout<T, HD>;
-  constexpr int NW = KeysCfg<T, HD>::NW, NT = 64 * NW, BM = 32, BKV = 32 * NW, TILE = BKV * HD;
+  constexpr int NW = KeysCfg<T, HD>::NW, NT = 64 * NW, BM = 32, BKV = 32 * NW, TILE = BKV * L::ROWB;
   constexpr int LOADS = 2 * 32 / L::RPI;  // of a wave's stage
-  __shared__ __align__(16) T ks0[TILE], ks1[TILE], vs0[TILE], vs1[TILE];
+  __shared__ __align__(16) char stages[2][2 * TILE];  // K, then V
   __shared__ int pg[PGCAP];
   __shared__ float2 wml[NW][32];
   __shared__ int bad, last;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div}, slots, may_many};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
@@ -939,38 +1040,46 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         pages.fill(fp, z * BKV, NT);
         __syncthreads();
         const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, fp, p.b.ps_div};
-        pages.load(a * BKV + wave * 32, ks0, vs0);
-        if (a + 1 < z) pages.load((a + 1) * BKV + wave * 32, ks1, vs1);
-#pragma unroll 1
-        for (int it = a; it < z; ++it) {
-          const bool second = (it - a) & 1;
-          // the wave's loads of this tile; those of the next one stay in flight
+        const lds_mem *mem = (const lds_mem *)&stages[0][0];
+        auto load = [&](int it) {
+          const lds_mem *k = mem + ((it - a) & 1) * 2 * TILE;
+          pages.load(it * BKV + wave * 32, k, k + TILE);
+        };
+        // The wave's loads of a tile have arrived; those of the next one stay in flight.
+        auto arrive = [&](int it) {
           if (it + 1 < z)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
           else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        };
+        auto leave = [&](int it) {  // the stage is read before it is loaded again
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (it + 2 < z) load(it + 2);
+        };
+        load(a);
+        if (a + 1 < z) load(a + 1);
+#pragma unroll 1
+        for (int it = a; it < z;) {
+          for (;;) {
+            arrive(it);
+            const int key0 = it * BKV + wave * 32;
+            if (it == t.t0 || key0 + 31 > pos_lo || key0 < last_first || seen.bad) break;
+            const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
+            if (!whole_blocks<T, HD, 1>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
+            leave(it);
+            if (++it == z) break;
+          }
+          if (it == z) break;
           const int key0 = it * BKV + wave * 32;
           if (key0 <= pos_hi && key0 + 32 > first_seen) {
-            if (key0 + 31 > pos_lo || key0 < last_first || seen.bad) {
-              const T *kt = second ? ks1 : ks0, *vt = second ? vs1 : vs0;
-              if (careful)
-                blocks<T, HD, CAREFUL, 1>(kt, vt, wave * 32, key0, q, st, p.scale_log2, lane, seen);
-              else
-                blocks<T, HD, SOME, 1>(kt, vt, wave * 32, key0, q, st, p.scale_log2, lane, seen);
-            } else if (second) {
-              blocks<T, HD, ALL, 1>(ks1, vs1, wave * 32, key0, q, st, p.scale_log2, lane, seen);
-            } else {
-              blocks<T, HD, ALL, 1>(ks0, vs0, wave * 32, key0, q, st, p.scale_log2, lane, seen);
-            }
-          }
-          // the stage is read before it is loaded again
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          if (it + 2 < z) {
-            if (second)
-              pages.load((it + 2) * BKV + wave * 32, ks1, vs1);
+            const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
+            if (careful)
+              block<T, HD, CAREFUL>(kt, kt + TILE, key0, q, st, p.scale_log2, lane, seen);
             else
-              pages.load((it + 2) * BKV + wave * 32, ks0, vs0);
+              block<T, HD, SOME>(kt, kt + TILE, key0, q, st, p.scale_log2, lane, seen);
           }
+          leave(it);
+          ++it;
         }
         a = z;
         __syncthreads();
@@ -979,12 +1088,10 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
       careful = true;
     }
 
-    // join the waves: O of wave w at 32 x HD floats w of ks0 and ks1
+    // join the waves: O of wave w at 32 x HD floats w of the stages
     const float lw = st.l + __shfl_xor(st.l, 32, 64);
-    auto osum = [&](int w) {
-      constexpr int PER = (int)(sizeof(T) * TILE / (32 * HD * 4));  // waves' O in one array
-      return (f32x4 *)(w < PER ? ks0 : ks1) + (w % PER) * 32 * (HD / 4);
-    };
+    auto osum = [&](int w) { return (f32x4 *)&stages[0][0] + w * 32 * (HD / 4); };
+    static_assert(NW * 32 * HD * 4 <= 4 * TILE, "O of all waves");
     {
       f32x4 *o = osum(wave);
 #pragma unroll
@@ -1048,7 +1155,6 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   // up to 32 rows to a sequence and KV head: the keys are shared out
   const bool keys = (int64_t)p.b.max_new * G <= 32;
   const int bm = keys ? 32 : 128;
-  p.least_keys = sizeof(T) == 2 ? 256 : 64;
   p.g_div = fast_div(G);
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
   const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 2)) : 0;  // two slots a workgroup
@@ -1059,6 +1165,14 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   const int64_t most = ((int64_t)p.b.n_rows * G / bm + p.b.n_seqs) * p.nkv;
   // (units of single tokens are all alike: stretches of them balance as well)
   const bool may_many = slots == 0 || (!keys && most >= (int64_t)MANY * slots);
+  // Workgroups that the work is worth.  keys: one to 256 keys (a tile of 128 takes a
+  // workgroup alone on its CU 1 us, its part in a join 0.1 us).  rows: a unit of c key
+  // tiles in p parts takes c / p tiles and a join of p parts, which is least at p =
+  // sqrt(c * tile / join), of all units together sqrt(units * work * tile / join); a tile
+  // takes 0.9 us (fp32: 4 us, of half the keys), a part in a join 1.2 us.
+  const int bkv = sizeof(T) == 2 ? 64 : 32;
+  p.spread_root = !keys;
+  p.spread = keys ? 1.0 / (256.0 * G) : (sizeof(T) == 2 ? 0.75 : 3.3) * (double)most / ((double)bkv * G);
   const int64_t grid = may_many ? most : slots;
   if (grid < 1) return hipSuccess;
   const dim3 g((unsigned)(grid < (1 << 24) ? grid : 1 << 24));

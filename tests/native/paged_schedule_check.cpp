@@ -26,7 +26,7 @@ int main() {
   for (int it = 0; it < 4000; ++it) {
     const int nkv = 1 + upto(7), G = 1 + upto(8), bm = it % 2 ? 32 : 128;
     const int window = upto(3) ? 0 : 1 + upto(3000);
-    const Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), fast_div(G)};
+    Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), 0, fast_div(G)};
     const int slots = 8 * (1 + upto(63)), seqs = 1 + upto(40);
     const int most_new = bm == 32 ? (32 / G > 0 ? 32 / G : 1) : 1 + upto(1 + upto(2000));
     std::vector<int> n(seqs), len(seqs);
@@ -35,6 +35,8 @@ int main() {
     for (int s = 0; s < seqs; ++s) {
       n[s] = upto(9) ? upto(most_new) : 0;
       len[s] = n[s] + upto(upto(3) ? 500 : 20000);
+      if (it % 5 == 0) len[s] = len[0] - n[0] + n[s], n[s] = n[s] ? n[0] : 0;  // alike, some idle
+      if (it % 5 == 0 && n[s]) len[s] = len[0];
       if (n[s] == 0) continue;
       total += sh.seq_work(n[s], len[s]);
       units += (int64_t)sh.work(n[s], len[s]).tiles * nkv;
@@ -65,10 +67,22 @@ int main() {
     if (seen != units) return fail("number of units", it);
     if (total == 0) continue;
     // dealt out
-    double share;
-    int n_wg;
-    deal(total, 256.0 * G, seqs * nkv, slots, share, n_wg);
+    double one = 0;
+    int heads = 0;
+    bool alike = true;
+    for (int s = 0; s < seqs; ++s) {
+      if (n[s] == 0) continue;
+      heads += nkv;
+      alike &= n[s] * G <= bm && (one == 0 || sh.seq_work(n[s], len[s]) == one * nkv);
+      one = sh.seq_work(n[s], len[s]) / nkv;
+    }
+    const Deal d = deal(total, total / (1.0 + upto(600)) / G, heads, alike ? one : 0, slots);
+    const double share = d.share;
+    const int n_wg = d.n_wg;
+    sh.pad = d.pad;
+    total += d.pad * heads;
     if (n_wg < 1 || n_wg > slots) return fail("more workgroups than slots", it);
+    if (n_wg * share < total) return fail("work that nobody gets", it);
     std::set<int> stretches;
     for (int b = 0; b < slots; ++b) {
       const int wg = stretch_of(b, n_wg);
