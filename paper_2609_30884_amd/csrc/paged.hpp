@@ -91,8 +91,7 @@ struct PagedAttn {
   int n_cu;
   // set by the launcher
   FastDiv g_div;       // by nq / nkv
-  double spread;       // workgroups wanted: work x spread, or its root
-  bool spread_root;
+  double per_wg;       // workgroups that a unit of work is worth (tiles of 32 rows)
 };
 hipError_t launch_paged_attn(hipStream_t s, bool f32, const PagedAttn &p);
 

@@ -34,6 +34,7 @@
 // is).  Many: one unit a workgroup, longest of a sequence first.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "paged.hpp"
@@ -43,7 +44,9 @@ namespace {
 
 constexpr float PSUM_MAX = 256.0f;  // a lane's sum of a block's probabilities that needs no new reference
 constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
-constexpr int MANY = 3;             // units per resident workgroup from which none is split
+constexpr int MANY = 3;             // rounds of units over the resident workgroups from which none is split
+constexpr int64_t SMALL_READS = 48 << 20;  // bytes of K and V up to which tiles of 32 rows do
+constexpr float SPLIT = 8.f;        // tiles that a part costs besides its keys
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -63,16 +66,17 @@ CRF_DEV s16x4 lds_tr(const lds_mem *p) { return __builtin_amdgcn_ds_read_tr16_b6
 // instruction that uses it, the others those between M0 and its use.
 //
 // One page: raw buffer resources of the K and V rows (loads past their end return zero).
+CRF_DEV uint32_t scalar(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 CRF_DEV u32x4 resource(const void *base, uint32_t bytes) {
   const uint64_t a = (uint64_t)base;
-  return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes, 0x00020000u};
+  return u32x4{scalar((uint32_t)a), scalar((uint32_t)(a >> 32) & 0xffffu), scalar(bytes), 0x00020000u};
 }
 CRF_DEV void dma_page(u32x4 kr, u32x4 vr, const lds_mem *kl, const lds_mem *vl, uint32_t ko, uint32_t vo) {
   asm volatile(
       "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
       "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds"
       :
-      : "s"(kl), "s"(vl), "v"(ko), "v"(vo), "s"(kr), "s"(vr)
+      : "s"(scalar((uint32_t)(uintptr_t)kl)), "s"(scalar((uint32_t)(uintptr_t)vl)), "v"(ko), "v"(vo), "s"(kr), "s"(vr)
       : "memory");
 }
 // Rows of their own: an address a lane.
@@ -81,7 +85,7 @@ CRF_DEV void dma_row(const char *k, const char *v, const lds_mem *kl, const lds_
       "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\t"
       "s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off"
       :
-      : "s"(kl), "s"(vl), "v"(k), "v"(v)
+      : "s"(scalar((uint32_t)(uintptr_t)kl)), "s"(scalar((uint32_t)(uintptr_t)vl)), "v"(k), "v"(v)
       : "memory");
 }
 
@@ -132,11 +136,14 @@ struct QFrag {
 // The keys that a lane's row sees: [lo, hi]; bad: some pages of the unit are out of
 // range, whose keys nobody sees.
 struct Seen {
-  int lo, hi, end;  // end: of the sequence
+  int lo, hi;
+  int all_from, all_to;  // keys that every row of the wave sees: [all_from, all_to)
+  int end;               // of the sequence
   bool bad;
   const int *pages;  // staged page numbers, the first of logical page `first`
   int first;
   FastDiv ps_div;
+  CRF_DEV bool all(int key0) const { return key0 >= all_from && key0 + 32 <= all_to; }
 };
 
 template <int HD>
@@ -324,10 +331,12 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
   f32x16 sc[1];
   scores<T, HD, 1>(kt, q, lane, sc);
   f32x16 &s = sc[0];
+  if (!seen.all(key0)) {
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int key = key0 + 8 * (v / 4) + 4 * g + v % 4;
-    if (key < seen.lo || key > seen.hi) s[v] = -INFINITY;
+    for (int v = 0; v < 16; ++v) {
+      const int key = key0 + 8 * (v / 4) + 4 * g + v % 4;
+      if (key < seen.lo || key > seen.hi) s[v] = -INFINITY;
+    }
   }
   if (seen.bad) {
 #pragma unroll 1
@@ -339,11 +348,14 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
           if (8 * (v / 4) + 4 * g + v % 4 == i) s[v] = -INFINITY;
     }
   }
-  float p[16], sum = 0.f;
+  float p[16], sum = INFINITY;
+  if (!__builtin_amdgcn_ballot_w64(st.ref == -INFINITY)) {
+    sum = 0.f;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    p[v] = fast_exp2(fmaf(s[v], c, -st.ref));
-    sum += p[v];
+    for (int v = 0; v < 16; ++v) {
+      p[v] = fast_exp2(fmaf(s[v], c, -st.ref));
+      sum += p[v];
+    }
   }
   if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {
     float mx = -INFINITY;
@@ -351,15 +363,22 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
     // only rows that need one: a row's result does not depend on the tile's others
+    if (sum == INFINITY && st.ref != -INFINITY) {  // (not formed above, for other rows' sake)
+      sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum += fast_exp2(fmaf(s[v], c, -st.ref));
+    }
     const float other = __shfl_xor(sum, 32, 64);
     const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
     const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
     const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
     const float base = ref == -INFINITY ? 0.f : ref;  // (a row that has seen no key yet)
     st.ref = ref;
-    st.l *= alpha;
+    if (__builtin_amdgcn_ballot_w64(st.l != 0.f)) {
+      st.l *= alpha;
 #pragma unroll
-    for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
+      for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
+    }
     sum = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -415,6 +434,7 @@ struct Shape {
   int over;                     // keys that a unit costs besides its own
   double pad;                   // and work added by the dealing
   FastDiv g_div;                // by G
+  float join;                   // joining a part, in tiles
 
   __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
   __host__ __device__ SeqWork work(int n, int len) const {
@@ -444,6 +464,23 @@ struct Shape {
   __host__ __device__ int last_key(const Task &t) const {  // of the tile's last row
     const int r = (t.tile + 1) * bm, rows = t.n * G;
     return t.len - t.n + by_g((r < rows ? r : rows) - 1);
+  }
+  // Whether `units` units of `total` work, the longest of a sequence of `longest` tokens,
+  // are dealt out whole, and else to how many workgroups their work goes.  In tiles of
+  // bkv keys: whole units take `rounds` times the longest one (a single sequence's, longest
+  // first, come out even from `MANY` rounds on), stretches the mean and what a part costs
+  // besides, SPLIT tiles.  A stretch of s tiles in units of c means s tiles and a join of
+  // c / s parts, `join` tiles each, one after the other: no shorter than sqrt(c join).
+  struct Plan {
+    bool whole;
+    double want;
+  };
+  __host__ __device__ Plan plan(double total, int units, int longest, int slots) const {
+    const int most = window > 0 && window + bm < longest ? window + bm : longest;
+    const float tile = (float)bkv * G, c = ((float)(most + over) * G + bm) / tile, mean = (float)total / tile / slots;
+    const int rounds = (units + slots - 1) / slots;
+    const float least = sqrtf(c * join);
+    return Plan{rounds >= MANY || rounds * c <= mean + SPLIT, total / (tile * (least > 1.f ? least : 1.f))};
   }
   // Unit i of the sequence's, whole: longest first, its KV heads next to each other.
   __host__ __device__ void whole(int i, Task &t) const {
@@ -533,13 +570,37 @@ CRF_DEV double lane_value(double v, int from) {
                                         (uint32_t)lane_value((int)u, from));
 }
 
+// Inclusive prefix over the wave by data-parallel primitives: within rows of 16 lanes,
+// then across them.
+template <typename F>
+CRF_DEV void wave_prefix(F step) {
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());  // row_shr:1
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // row_bcast:15
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // row_bcast:31
+}
+// The value of the lane that step C names, zero where it names none.
+template <int C, int ROWS>
+CRF_DEV int from_lane(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, C, ROWS, 0xf, false);
+}
+template <int C, int ROWS>
+CRF_DEV double from_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)from_lane<C, ROWS>((int)(u >> 32)) << 32 |
+                                        (uint32_t)from_lane<C, ROWS>((int)u));
+}
+
 // What a workgroup computes, unit after unit.  Every wave works it out for itself,
 // 64 sequences at a time, so that nothing waits for a barrier.
 struct Schedule {
   const PagedAttn &p;
   Shape sh;
   int slots;
-  bool many;  // units dealt out whole, gridDim.x apart; else stretches of work
+  bool sizes;         // units differ (tiles of 128 rows): whether they are split is decided here
+  bool many = false;  // units dealt out whole, gridDim.x apart; else stretches of work
   bool dealt = false;
   int wg = 0;
   double share = 0, at = -1, end = 0;  // many: next unit and their number; else the stretch [at, end) of all work
@@ -549,26 +610,28 @@ struct Schedule {
   struct Lane {  // a lane's sequence, its work and where that begins
     int s, start, n, len;
     double v, from;
+    int units, longest;
   };
 
   // Prefix sums over the sequences of their work (units: of their units), of which the
   // total is returned; finds the sequence that holds position x, and leaves each lane
-  // its last sequence.
-  CRF_DEV double pass(double x, bool units, Lane &q) {
+  // its last sequence and, when `sizes`, its sequences' units and longest.
+  CRF_DEV double pass(double x, bool units, Lane &q, bool sizes = false) {
     const int lane = threadIdx.x % 64;
     double done = 0;
+    q.units = q.longest = 0;
 #pragma unroll 1
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += 64) {
       q.s = s0 + lane;
       q.start = q.len = 0;
       q.n = q.s < p.b.n_seqs ? seq_new(p.b, q.s, q.start, q.len) : 0;
       q.v = q.n > 0 ? sh.seq_work(q.n, q.len, units) : 0;
-      double sum = q.v;
-#pragma unroll 1
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += y;
+      if (sizes && q.n > 0) {
+        q.units += sh.work(q.n, q.len).tiles * sh.nkv;
+        q.longest = max(q.longest, q.len);
       }
+      double sum = q.v;
+      wave_prefix([&](auto c, auto rows) { sum += from_lane<c(), rows()>(sum); });
       q.from = done + sum - q.v;
       hold(x, q);
       done += lane_value(sum, 63);
@@ -594,16 +657,26 @@ struct Schedule {
     if (!dealt) {
       dealt = true;
       Lane q;
-      double total = pass(-1, many, q);
-      if (many && total < (double)MANY * slots) {  // not that many
-        many = false;
-        total = pass(-1, false, q);
+      double total = pass(-1, false, q, sizes);
+      if (total == 0) return false;
+      double want;
+      many = slots == 0;
+      if (sizes) {
+        wave_prefix([&](auto c, auto rows) {
+          q.units += from_lane<c(), rows()>(q.units);
+          q.longest = max(q.longest, from_lane<c(), rows()>(q.longest));
+        });
+        const int units = lane_value(q.units, 63);
+        const Shape::Plan plan = sh.plan(total, units, lane_value(q.longest, 63), slots);
+        many |= plan.whole;
+        want = plan.want;
+        end = units;
+      } else {
+        want = total * p.per_wg;
       }
       if (many) {
         at = blockIdx.x;
-        end = total;
       } else {
-        if (__builtin_amdgcn_readfirstlane(total == 0)) return false;
         // sequences of one tile and one length?
         double one = 0;
         int heads = p.b.n_seqs * sh.nkv;
@@ -613,7 +686,6 @@ struct Schedule {
           heads = __popcll(active) * sh.nkv;
           if (!__builtin_amdgcn_ballot_w64(q.v > 0 && (q.v != v || q.n * sh.G > sh.bm))) one = v / sh.nkv;
         }
-        const double want = p.spread_root ? (double)sqrtf((float)(total * p.spread)) : total * p.spread;
         const Deal d = deal(total, want, heads, one, slots);
         share = lane_value(d.share, 0);
         sh.pad = lane_value(d.pad, 0);
@@ -848,7 +920,7 @@ struct Pages {
 // ---------------------------------------------------------------- tiles of 128 rows
 
 template <typename T, int HD, bool UNI>
-__global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots, bool may_many) {
+__global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots) {
   using L = Layout<T, HD>;
   constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW, BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * L::ROWB;
   __shared__ __align__(16) char stages[2][2 * TILE];  // K, then V
@@ -857,7 +929,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f}, slots, true};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
@@ -924,7 +996,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         if (it == t.t1) break;
         const int kt0 = it * BKV;
         if (wave * 32 < rows && kt0 <= pos_hi && kt0 + BKV > first_seen) {
-          const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, pages.first, p.b.ps_div};
+          const Seen seen{pos > far ? pos - far : 0, pos, last_first, whole_to, t.len, bad != 0, pg, pages.first, p.b.ps_div};
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
 #pragma unroll 1
           for (int kb = 0; kb < BKV; kb += 32)
@@ -994,7 +1066,7 @@ struct KeysCfg {
 
 template <typename T, int HD, bool UNI>
 __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_CU)) void attn_keys_kernel(
-    const PagedAttn p, int slots, bool may_many) {
+    const PagedAttn p, int slots) {
   using L = Layout<T, HD>;
   constexpr int NW = KeysCfg<T, HD>::NW, NT = 64 * NW, BM = 32, BKV = 32 * NW, TILE = BKV * L::ROWB;
   constexpr int LOADS = 2 * 32 / L::RPI;  // of a wave's stage
@@ -1005,7 +1077,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div}, slots, may_many};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, 0}, slots, slots == 0};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
@@ -1039,7 +1111,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         const int z = tiles < t.t1 ? (int)tiles : t.t1;
         pages.fill(fp, z * BKV, NT);
         __syncthreads();
-        const Seen seen{pos > far ? pos - far : 0, pos, t.len, bad != 0, pg, fp, p.b.ps_div};
+        const Seen seen{pos > far ? pos - far : 0, pos, last_first, pos_lo + 1, t.len, bad != 0, pg, fp, p.b.ps_div};
         const lds_mem *mem = (const lds_mem *)&stages[0][0];
         auto load = [&](int it) {
           const lds_mem *k = mem + ((it - a) & 1) * 2 * TILE;
@@ -1063,7 +1135,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
           for (;;) {
             arrive(it);
             const int key0 = it * BKV + wave * 32;
-            if (it == t.t0 || key0 + 31 > pos_lo || key0 < last_first || seen.bad) break;
+            if (it == t.t0 || !seen.all(key0) || seen.bad) break;
             const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
             if (!whole_blocks<T, HD, 1>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
             leave(it);
@@ -1152,8 +1224,14 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
 template <typename T, int HD, bool UNI>
 hipError_t launch(hipStream_t s, PagedAttn p) {
   const int G = p.nq / p.nkv;
-  // up to 32 rows to a sequence and KV head: the keys are shared out
-  const bool keys = (int64_t)p.b.max_new * G <= 32;
+  // Tiles of 32 rows for up to 32 rows to a sequence and KV head, and where all of them
+  // together read so few keys (as far as the host can tell) that four times the reads of
+  // K and V cost less than the parts of long units: six fp32 chunks of up to 64 tokens
+  // over 1500 32 -> 27 us.
+  const int64_t row_tiles = ((int64_t)p.b.n_rows * G / 32 + p.b.n_seqs) * p.nkv;
+  const int64_t longest = std::min<int64_t>((int64_t)p.b.max_pages * p.b.page_size, (int64_t)1 << 24);
+  const bool keys = (int64_t)p.b.max_new * G <= 32 ||
+                    (row_tiles < (1 << 16) && row_tiles * longest * 2 * HD * (int)sizeof(T) <= SMALL_READS);
   const int bm = keys ? 32 : 128;
   p.g_div = fast_div(G);
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
@@ -1163,23 +1241,15 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   slots = slots / 8 * 8;
   // (a sequence's last tile may be short)
   const int64_t most = ((int64_t)p.b.n_rows * G / bm + p.b.n_seqs) * p.nkv;
-  // (units of single tokens are all alike: stretches of them balance as well)
-  const bool may_many = slots == 0 || (!keys && most >= (int64_t)MANY * slots);
-  // Workgroups that the work is worth.  keys: one to 256 keys (a tile of 128 takes a
-  // workgroup alone on its CU 1 us, its part in a join 0.1 us).  rows: a unit of c key
-  // tiles in p parts takes c / p tiles and a join of p parts, which is least at p =
-  // sqrt(c * tile / join), of all units together sqrt(units * work * tile / join); a tile
-  // takes 0.9 us (fp32: 4 us, of half the keys), a part in a join 1.2 us.
-  const int bkv = sizeof(T) == 2 ? 64 : 32;
-  p.spread_root = !keys;
-  p.spread = keys ? 1.0 / (256.0 * G) : (sizeof(T) == 2 ? 0.75 : 3.3) * (double)most / ((double)bkv * G);
-  const int64_t grid = may_many ? most : slots;
+  // (a tile of 128 keys takes a workgroup alone on its CU 1 us, a part in a join 0.1 us)
+  p.per_wg = 1.0 / (256.0 * G);
+  const int64_t grid = slots == 0 || most >= (int64_t)MANY * slots ? most : slots;
   if (grid < 1) return hipSuccess;
   const dim3 g((unsigned)(grid < (1 << 24) ? grid : 1 << 24));
   if (keys)
-    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots, may_many);
+    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots);
   else
-    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI>), g, dim3(256), 0, s, p, slots, may_many);
+    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI>), g, dim3(256), 0, s, p, slots);
   return hipGetLastError();
 }
 
