@@ -46,6 +46,7 @@ constexpr float PSUM_MAX = 256.0f;  // a lane's sum of a block's probabilities t
 constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
 constexpr int MANY = 3;             // rounds of units over the resident workgroups from which none is split
 constexpr int64_t SMALL_READS = 48 << 20;  // bytes of K and V up to which tiles of 32 rows do
+constexpr int SLIVER = 2;           // fewer tiles are no part of their own
 constexpr float SPLIT = 8.f;        // tiles that a part costs besides its keys
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -493,7 +494,8 @@ struct Shape {
   }
   // What workgroup wg, whose stretch ends at `end`, computes from position `at` of
   // all work on, `at` being in the sequence, whose work begins at seq_base; returns
-  // where it stops (the end of the unit or of the stretch).
+  // where it stops (the end of the unit or of the stretch).  It has no part in the unit
+  // when t.part is none of the unit's parts.
   __host__ __device__ double part_at(double at, double end, double share, int wg, double seq_base, Task &t) const {
     const SeqWork w = work(t.n, t.len);
     const double one = w.before(w.tiles), off = at - seq_base;
@@ -511,12 +513,17 @@ struct Shape {
                  u1 = u0 + cost;
     const double stop = u1 < end ? u1 : end;
     const int k0 = first_key(t) / bkv, k = last_key(t) / bkv + 1 - k0;
-    // (both neighbours of a border find it by the same arithmetic)
-    t.t0 = k0 + (int)quotient((at - u0) * k, cost);
-    t.t1 = stop == u1 ? k0 + k : k0 + (int)quotient((stop - u0) * k, cost);
+    // First key tile of workgroup w's part (both neighbours of a border find it by the same
+    // arithmetic).  A first or last part of fewer than SLIVER tiles goes to its neighbour.
+    auto border = [&](int w) { return (int)quotient((w * share - u0) * k, cost); };
+    int last = (int)quotient(u1 - 1, share);
     t.owner = (int)quotient(u0, share);
-    t.parts = (int)quotient(u1 - 1, share) - t.owner + 1;
+    if (t.owner < last && border(t.owner + 1) < SLIVER) ++t.owner;
+    if (t.owner < last && k - border(last) < SLIVER) --last;
+    t.parts = last - t.owner + 1;
     t.part = wg - t.owner;
+    t.t0 = k0 + (t.part == 0 ? 0 : border(wg));
+    t.t1 = k0 + (t.part == t.parts - 1 ? k : border(wg + 1));
     return stop;
   }
 };
@@ -706,34 +713,38 @@ struct Schedule {
         }
       }
     }
-    if (__builtin_amdgcn_readfirstlane(at >= end)) return false;
-    if (many) {
-      Lane q;
-      pass(at, true, q);
-    } else {
 #pragma unroll 1
-      while (__builtin_amdgcn_readfirstlane(at >= base + work)) {  // (some sequence holds `at`)
-        base += work;
-        n = seq_new(p.b, ++seq, start, len);
-        work = n > 0 ? sh.seq_work(n, len) : 0;
+    for (;;) {
+      if (__builtin_amdgcn_readfirstlane(at >= end)) return false;
+      if (many) {
+        Lane q;
+        pass(at, true, q);
+      } else {
+#pragma unroll 1
+        while (__builtin_amdgcn_readfirstlane(at >= base + work)) {  // (some sequence holds `at`)
+          base += work;
+          n = seq_new(p.b, ++seq, start, len);
+          work = n > 0 ? sh.seq_work(n, len) : 0;
+        }
       }
-    }
-    t.seq = __builtin_amdgcn_readfirstlane(seq);
-    t.start = __builtin_amdgcn_readfirstlane(start);
-    t.n = __builtin_amdgcn_readfirstlane(n);
-    t.len = __builtin_amdgcn_readfirstlane(len);
-    if (many) {
-      sh.whole(__builtin_amdgcn_readfirstlane((int)(at - base)), t);
-      at += gridDim.x;
-    } else {
+      t.seq = __builtin_amdgcn_readfirstlane(seq);
+      t.start = __builtin_amdgcn_readfirstlane(start);
+      t.n = __builtin_amdgcn_readfirstlane(n);
+      t.len = __builtin_amdgcn_readfirstlane(len);
+      if (many) {
+        sh.whole(__builtin_amdgcn_readfirstlane((int)(at - base)), t);
+        at += gridDim.x;
+        break;
+      }
       at = lane_value(sh.part_at(at, end, share, wg, base, t), 0);
+      t.part = __builtin_amdgcn_readfirstlane(t.part);
+      if (t.part >= 0 && t.part < __builtin_amdgcn_readfirstlane(t.parts)) break;
     }
     t.kvh = __builtin_amdgcn_readfirstlane(t.kvh);
     t.tile = __builtin_amdgcn_readfirstlane(t.tile);
     t.t0 = __builtin_amdgcn_readfirstlane(t.t0);
     t.t1 = __builtin_amdgcn_readfirstlane(t.t1);
     t.parts = __builtin_amdgcn_readfirstlane(t.parts);
-    t.part = __builtin_amdgcn_readfirstlane(t.part);
     t.owner = __builtin_amdgcn_readfirstlane(t.owner);
     return true;
   }

@@ -109,8 +109,9 @@ int main() {
         const double stop = sh.part_at(at, end, share, wg, base, t);
         if (stop <= at || stop > end) return fail("no progress", it);
         at = stop;
+        if (t.part < 0 || t.part >= t.parts) continue;  // a sliver, which a neighbour takes
         unit[{s, t.kvh, t.tile}].push_back(t);
-        if (t.part < 0 || t.part >= t.parts || t.owner < 0 || t.owner + t.parts > n_wg) return fail("part number", it);
+        if (t.owner < 0 || t.owner + t.parts > n_wg) return fail("part number", it);
         if (t.parts > 1) {
           const int sl = part_slot(t.owner, t.part);
           if (sl < 0 || sl >= 2 * slots || !slot.insert(sl).second) return fail("two partials in a slot", it);
