@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace crf {
@@ -32,6 +34,23 @@ inline FastDiv fast_div(int d) {
   return FastDiv{(uint32_t)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
 }
 CRF_DEV int div_by(int n, FastDiv f) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
+
+// Inclusive prefix over the wave by data-parallel primitives: within rows of 16 lanes,
+// then across them.
+template <typename F>
+CRF_DEV void wave_prefix(F step) {
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());  // row_shr:1
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // row_bcast:15
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // row_bcast:31
+}
+// The value of the lane that step C names, zero where it names none.
+template <int C, int ROWS>
+CRF_DEV int from_lane(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, C, ROWS, 0xf, false);
+}
 
 // Sequences with their new tokens and the pages they own, in one layer's pools.
 struct PagedBatch {

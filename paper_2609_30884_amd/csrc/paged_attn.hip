@@ -577,22 +577,6 @@ CRF_DEV double lane_value(double v, int from) {
                                         (uint32_t)lane_value((int)u, from));
 }
 
-// Inclusive prefix over the wave by data-parallel primitives: within rows of 16 lanes,
-// then across them.
-template <typename F>
-CRF_DEV void wave_prefix(F step) {
-  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());  // row_shr:1
-  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
-  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
-  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
-  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // row_bcast:15
-  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // row_bcast:31
-}
-// The value of the lane that step C names, zero where it names none.
-template <int C, int ROWS>
-CRF_DEV int from_lane(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, C, ROWS, 0xf, false);
-}
 template <int C, int ROWS>
 CRF_DEV double from_lane(double v) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);

@@ -23,7 +23,7 @@ int main() {
   std::mt19937 rng(7);
   auto upto = [&](int n) { return (int)(rng() % (unsigned)(n + 1)); };
   int checked = 0;
-  for (int it = 0; it < 4000; ++it) {
+  for (int it = 0; it < 4200; ++it) {
     const int nkv = 1 + upto(7), G = 1 + upto(8), bm = it % 2 ? 32 : 128;
     const int window = upto(3) ? 0 : 1 + upto(3000);
     Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), 0, fast_div(G), 1.f};
