@@ -51,6 +51,12 @@ template <int C, int ROWS>
 CRF_DEV int from_lane(int v) {
   return __builtin_amdgcn_update_dpp(0, v, C, ROWS, 0xf, false);
 }
+template <int C, int ROWS>
+CRF_DEV double from_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)from_lane<C, ROWS>((int)(u >> 32)) << 32 |
+                                        (uint32_t)from_lane<C, ROWS>((int)u));
+}
 
 // Sequences with their new tokens and the pages they own, in one layer's pools.
 struct PagedBatch {

@@ -577,13 +577,6 @@ CRF_DEV double lane_value(double v, int from) {
                                         (uint32_t)lane_value((int)u, from));
 }
 
-template <int C, int ROWS>
-CRF_DEV double from_lane(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  return __builtin_bit_cast(double, (uint64_t)(uint32_t)from_lane<C, ROWS>((int)(u >> 32)) << 32 |
-                                        (uint32_t)from_lane<C, ROWS>((int)u));
-}
-
 // What a workgroup computes, unit after unit.  Every wave works it out for itself,
 // 64 sequences at a time, so that nothing waits for a barrier.
 struct Schedule {
