@@ -21,7 +21,7 @@
 // XOR-swizzled by row.
 //
 // The reference ref is no running maximum: a block's probabilities are formed with
-// the one there is, and only where a lane's sum passes 2^8 is the maximum taken and
+// the one there is, and only where a lane's sum passes 2^16 is the maximum taken and
 // O rescaled.  It starts at minus infinity, which makes the first block that a row
 // sees take that path.  Scores, sums and O are fp32; the probabilities are rounded
 // to the storage type for the second product, as MFMA needs them (bf16: 2^-8
@@ -42,7 +42,7 @@
 namespace crf {
 namespace {
 
-constexpr float PSUM_MAX = 256.0f;  // a lane's sum of a block's probabilities that needs no new reference
+constexpr float PSUM_MAX = 65536.0f; // a lane's sum of a block's probabilities that needs no new reference
 constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
 constexpr int MANY = 3;             // rounds of units over the resident workgroups from which none is split
 constexpr int64_t SMALL_READS = 48 << 20;  // bytes of K and V up to which tiles of 32 rows do
@@ -206,10 +206,12 @@ CRF_DEV void scores(const lds_mem *kt, const QFrag<T, HD> &q, int lane, f32x16 (
 }
 
 // How a block of keys is taken.  ALL: every row sees all of it and keeps its reference.
-// SOME: some row does not see some key, or needs another reference.  CAREFUL: the same where a value that is not finite may belong to
-// a key that some row does not see: the product would multiply it by that row's
-// weight zero, so such values are taken out of the product and added where the weight
-// is not zero.  (Units run with SOME first, and again if their result is not finite.)
+// SOME: some row does not see some key, or needs another reference.  CAREFUL: a value
+// that is not finite may belong to a key that some row does not see: the product would
+// multiply it by that row's weight zero, so such values are taken out of the product and
+// added where the weight is not zero; and the reference is the maximum, so that large
+// values times weights of up to PSUM_MAX stay in range.  (Units run without it first,
+// and again if their result is not finite.)
 enum Take { ALL, SOME, CAREFUL };
 
 // O += P V for the probabilities p of 32 keys (V rows from vt on).
@@ -328,6 +330,7 @@ CRF_DEV bool whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, H
 template <typename T, int HD, Take TAKE>
 CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
                    int lane, const Seen &seen) {
+  constexpr float most = TAKE == CAREFUL ? 16.f : PSUM_MAX;
   const int g = lane / 32;
   f32x16 sc[1];
   scores<T, HD, 1>(kt, q, lane, sc);
@@ -358,7 +361,7 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
       sum += p[v];
     }
   }
-  if (__builtin_amdgcn_ballot_w64(!(sum <= PSUM_MAX))) {
+  if (__builtin_amdgcn_ballot_w64(!(sum <= most))) {
     float mx = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
@@ -370,7 +373,7 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
       for (int v = 0; v < 16; ++v) sum += fast_exp2(fmaf(s[v], c, -st.ref));
     }
     const float other = __shfl_xor(sum, 32, 64);
-    const bool raise = !(sum <= PSUM_MAX) || !(other <= PSUM_MAX);
+    const bool raise = !(sum <= most) || !(other <= most);
     const float ref = raise ? fmaxf(st.ref, mx) : st.ref;
     const float alpha = ref == -INFINITY ? 1.f : fast_exp2(st.ref - ref);
     const float base = ref == -INFINITY ? 0.f : ref;  // (a row that has seen no key yet)
@@ -976,7 +979,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         for (;;) {
           arrive(it);
           const int kt0 = it * BKV;
-          if (it == t.t0 || kt0 + BKV > whole_to || kt0 < last_first || bad) break;
+          if (it == t.t0 || kt0 + BKV > whole_to || kt0 < last_first || bad || careful) break;
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
           if (!whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
           if (++it == t.t1) break;
@@ -1123,7 +1126,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
           for (;;) {
             arrive(it);
             const int key0 = it * BKV + wave * 32;
-            if (it == t.t0 || !seen.all(key0) || seen.bad) break;
+            if (it == t.t0 || !seen.all(key0) || seen.bad || careful) break;
             const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
             if (!whole_blocks<T, HD, 1>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
             leave(it);

@@ -126,6 +126,23 @@ def test_scale_and_strides(dtype):
     assert torch.equal(b.q.reshape(b.n_rows, 256), out[:, :256])
 
 
+@pytest.mark.parametrize("dtype,hd,seqs", [(BF, 128, [(40, 2000), (100, 900)]), (BF, 64, [(1, 2000), (2, 500)]),
+                                           (F32, 64, [(90, 1500)])])
+def test_values_near_the_largest(dtype, hd, seqs):
+    """Weights that rise by 2^15 along the keys times values of 2^109: the sums pass the
+    range unless the reference follows the scores."""
+    from tests.paged import Batch
+    print(f"[case] large values {dtype} hd {hd}", flush=True)
+    b = Batch(seqs, 4, 2, hd, _dt(dtype), seed=21)
+    b.q.fill_(1.0)
+    for s, t in enumerate(b.total):
+        pg, sl = b.places(s)
+        rise = torch.arange(t, device="cuda") * (15 * math.log(2) / t) * hd ** -0.5
+        b.k_pool[1, pg, :, sl] = rise[:, None, None].to(b.dtype).expand(t, 2, hd)
+    b.v_pool.copy_(b.v_pool.abs() * 2.0 ** 109)
+    _check(b, "large values")
+
+
 @pytest.mark.parametrize("dtype,nq,nkv", [(BF, 12, 2), (F32, 4, 2)])
 @pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
 def test_what_a_row_does_not_see(dtype, nq, nkv, odd):
