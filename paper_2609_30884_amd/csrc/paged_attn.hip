@@ -439,6 +439,7 @@ struct Shape {
   double pad;                   // and work added by the dealing
   FastDiv g_div;                // by G
   float join;                   // joining a part, in tiles
+  bool lead = false;            // `over` lies before a unit's keys, else among them
 
   __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
   __host__ __device__ SeqWork work(int n, int len) const {
@@ -518,10 +519,14 @@ struct Shape {
     const int k0 = first_key(t) / bkv, k = last_key(t) / bkv + 1 - k0;
     // First key tile of workgroup w's part (both neighbours of a border find it by the same
     // arithmetic).  A first or last part of fewer than SLIVER tiles goes to its neighbour.
-    auto border = [&](int w) { return (int)quotient((w * share - u0) * k, cost); };
+    const double ahead = lead ? w.over : 0;
+    auto border = [&](int w) {
+      const double x = w * share - u0 - ahead;
+      return x > 0 ? (int)quotient(x * k, cost - ahead) : 0;
+    };
     int last = (int)quotient(u1 - 1, share);
     t.owner = (int)quotient(u0, share);
-    if (t.owner < last && border(t.owner + 1) < SLIVER) ++t.owner;
+    while (t.owner < last && border(t.owner + 1) < SLIVER) ++t.owner;
     if (t.owner < last && k - border(last) < SLIVER) --last;
     t.parts = last - t.owner + 1;
     t.part = wg - t.owner;
@@ -920,7 +925,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f}, slots, true};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f, true}, slots, true};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees

@@ -26,7 +26,7 @@ int main() {
   for (int it = 0; it < 4200; ++it) {
     const int nkv = 1 + upto(7), G = 1 + upto(8), bm = it % 2 ? 32 : 128;
     const int window = upto(3) ? 0 : 1 + upto(3000);
-    Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), 0, fast_div(G), 1.f};
+    Shape sh{G, nkv, window, bm, bm == 32 ? 128 : 64, upto(600), 0, fast_div(G), 1.f, it % 3 == 0};
     const int slots = 8 * (1 + upto(63)), seqs = 1 + upto(40);
     const int most_new = bm == 32 ? (32 / G > 0 ? 32 / G : 1) : 1 + upto(1 + upto(2000));
     std::vector<int> n(seqs), len(seqs);
