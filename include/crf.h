@@ -374,7 +374,8 @@ typedef struct {
 
 /* Host only.  scaling NULL: none.  Errors: INVALID_ARG (NULL, unknown layout or
  * scaling), UNSUPPORTED (rotary_dim no multiple of 16 in [0, 128]), SHAPE
- * (theta, factor, mscale, original_len or turns out of range). */
+ * (theta, factor, mscale, original_len or turns out of range, a frequency that is
+ * not finite). */
 crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, double theta,
                          const crf_rope_scaling *scaling);
 
@@ -389,7 +390,8 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
  * A token on a page out of range raises error bit 0 and is not appended (its q is
  * still rotated).
  * Errors: INVALID_ARG, SHAPE, RANGE (layer), UNSUPPORTED (rotary_dim above
- * head_dim or no multiple of 16, more than 2^30 tokens a table or rows x heads). */
+ * head_dim or no multiple of 16, more than 2^30 tokens a table, rows x query heads
+ * or sequences x query heads). */
 crf_status crf_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq_batch *batch,
                            const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                            const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride,

@@ -11,7 +11,7 @@ using namespace crf;
 
 namespace {
 
-constexpr int64_t MAX_KEYS = (int64_t)1 << 30;  // tokens that a block table may hold; rows x query heads
+constexpr int64_t MAX_KEYS = (int64_t)1 << 30;  // tokens that a block table may hold; rows, sequences x query heads
 
 bool aligned4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
 
@@ -65,6 +65,8 @@ crf_status check_batch(crf_context *ctx, const crf_seq_batch *b, const crf_page_
     return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: block tables of more than 2^30 tokens", what);
   if ((int64_t)b->n_rows * ctx->dims.n_q_heads > MAX_KEYS)
     return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: more than 2^30 rows x query heads", what);
+  if ((int64_t)b->n_seqs * ctx->dims.n_q_heads > MAX_KEYS)
+    return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: more than 2^30 sequences x query heads", what);
   if (b->n_seqs == 0 || b->n_rows == 0) return CRF_OK;
   if (!b->row_start || !b->length || !b->block_tables)
     return fail(ctx, CRF_ERR_INVALID_ARG, "%s: row_start, length and block_tables must be non-NULL", what);
@@ -174,7 +176,7 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
     return fail(nullptr, CRF_ERR_INVALID_ARG, "%s: unknown scaling %d", what, sc.kind);
   if (sc.kind != CRF_ROPE_NONE && (!(sc.factor > 0) || !isfinite(sc.factor)))
     return fail(nullptr, CRF_ERR_SHAPE, "%s: the scaling factor must be positive", what);
-  if (!(sc.mscale >= 0) || !isfinite(sc.mscale))
+  if (!(sc.mscale >= 0) || !isfinite((float)sc.mscale))
     return fail(nullptr, CRF_ERR_SHAPE, "%s: mscale must be finite and >= 0", what);
   const double low = sc.low_turns > 0 ? sc.low_turns : 1.0, high = sc.high_turns > 0 ? sc.high_turns : 32.0;
   if (sc.kind == CRF_ROPE_PARTS && (!(sc.original_len >= 1) || !(high > low)))
@@ -195,6 +197,7 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
       const double keep = fmin(1.0, fmax(0.0, (turns - low) / (high - low)));
       f *= (1 - keep) / sc.factor + keep;
     }
+    if (!isfinite(f)) return fail(nullptr, CRF_ERR_SHAPE, "%s: the frequency of pair %d is not finite", what, i);
     out->freq[i] = f;
   }
   return CRF_OK;
@@ -259,7 +262,7 @@ crf_status crf_paged_attention(crf_context *ctx, const crf_seq_batch *batch, con
   if (st == CRF_OK) st = check_batch(ctx, batch, *pool, what);
   if (st != CRF_OK) return st;
   const crf_model_dims &d = ctx->dims;
-  if (!(scale >= 0.f) || !isfinite(scale))
+  if (!(scale >= 0.f) || !isfinite(1.45f * scale))
     return fail(ctx, CRF_ERR_SHAPE, "%s: scale must be finite and >= 0 (0: 1/sqrt(head_dim))", what);
   if (window < 0) return fail(ctx, CRF_ERR_SHAPE, "%s: window must be >= 0 (0: every key)", what);
   if (batch->n_seqs == 0 || batch->n_rows == 0) return CRF_OK;

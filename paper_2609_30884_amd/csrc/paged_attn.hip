@@ -652,7 +652,6 @@ struct Schedule {
       double total = pass(-1, false, q, sizes);
       if (total == 0) return false;
       double want;
-      many = slots == 0;
       if (sizes) {
         wave_prefix([&](auto c, auto rows) {
           q.units += from_lane<c(), rows()>(q.units);
@@ -660,7 +659,7 @@ struct Schedule {
         });
         const int units = lane_value(q.units, 63);
         const Shape::Plan plan = sh.plan(total, units, lane_value(q.longest, 63), slots);
-        many |= plan.whole;
+        many = plan.whole;
         want = plan.want;
         end = units;
       } else {
@@ -1073,7 +1072,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, 0}, slots, slots == 0};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, 0}, slots, false};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
@@ -1231,17 +1230,17 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   const int bm = keys ? 32 : 128;
   p.g_div = fast_div(G);
   const int resident = p.n_cu * (keys ? KeysCfg<T, HD>::WG_PER_CU : 2);
-  const int64_t room = p.part ? p.part_floats / (2 * bm * (HD + 2)) : 0;  // two slots a workgroup
+  const int64_t room = p.part_floats / (2 * bm * (HD + 2));  // two slots a workgroup
   int slots = (int)(room < resident ? room : resident);
   if (slots > PAGED_TICKETS) slots = PAGED_TICKETS;
   slots = slots / 8 * 8;
+  if (slots < 8) return hipErrorOutOfMemory;  // (no context is that small)
   // (a sequence's last tile may be short)
   const int64_t most = ((int64_t)p.b.n_rows * G / bm + p.b.n_seqs) * p.nkv;
   // (a tile of 128 keys takes a workgroup alone on its CU 1 us, a part in a join 0.1 us)
   p.per_wg = 1.0 / (256.0 * G);
-  const int64_t grid = slots == 0 || most >= (int64_t)MANY * slots ? most : slots;
-  if (grid < 1) return hipSuccess;
-  const dim3 g((unsigned)(grid < (1 << 24) ? grid : 1 << 24));
+  const int64_t grid = !keys && most >= (int64_t)MANY * slots ? most : slots;
+  const dim3 g((unsigned)(grid < MOST_GROUPS ? grid : MOST_GROUPS));
   if (keys)
     hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots);
   else

@@ -323,29 +323,32 @@ __global__ __launch_bounds__(PNT) void extend_kernel(const PageMap m, const int3
 
 // ---------------------------------------------------------------- freeing
 
-__global__ __launch_bounds__(CNT) void free_kernel(const PageMap m, const int32_t *seqs) {
+__global__ __launch_bounds__(CNT) void free_kernel(const PageMap m, int n, const int32_t *seqs) {
   __shared__ int len_s;
-  const int s = seqs[blockIdx.x];
-  if (s < 0 || s >= m.n_seqs) {
-    if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
-    return;
-  }
-  // (a sequence that is named twice is freed by whoever takes its length)
-  if (threadIdx.x == 0) len_s = atomicExch(&m.lengths[s], 0);
-  __syncthreads();
-  const int len = len_s;
-  if (len < 0 || (int64_t)len > (int64_t)m.max_pages * m.page_size) {
-    if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
-    return;
-  }
-  const int held = pages_of(len, m.page_size);
-  for (int j = threadIdx.x; j < held; j += CNT) {
-    const int e = m.tables[(int64_t)s * m.table_stride + j];
-    if (e < 0 || e >= m.n_pages) {
-      atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
-    } else if (atomicSub(&m.refs[e], 1) <= 0) {  // held by nobody
-      atomicAdd(&m.refs[e], 1);
-      atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int s = seqs[i];
+    if (s < 0 || s >= m.n_seqs) {
+      if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+      continue;
+    }
+    __syncthreads();  // (the length before has been read)
+    // (a sequence that is named twice is freed by whoever takes its length)
+    if (threadIdx.x == 0) len_s = atomicExch(&m.lengths[s], 0);
+    __syncthreads();
+    const int len = len_s;
+    if (len < 0 || (int64_t)len > (int64_t)m.max_pages * m.page_size) {
+      if (threadIdx.x == 0) atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+      continue;
+    }
+    const int held = pages_of(len, m.page_size);
+    for (int j = threadIdx.x; j < held; j += CNT) {
+      const int e = m.tables[(int64_t)s * m.table_stride + j];
+      if (e < 0 || e >= m.n_pages) {
+        atomicOr(m.err, (int)CRF_DEVERR_BLOCK_TABLE);
+      } else if (atomicSub(&m.refs[e], 1) <= 0) {  // held by nobody
+        atomicAdd(&m.refs[e], 1);
+        atomicOr(m.err, (int)CRF_DEVERR_BATCH);
+      }
     }
   }
 }
@@ -448,7 +451,7 @@ hipError_t launch_pages_copy(hipStream_t s, const PagePools &from, const PagePoo
   if (n <= 0 || layers <= 0) return hipSuccess;
   CopyArgs a = copy_args(from, to, layers, bytes, n, err);
   const int64_t blocks = (int64_t)n * a.blocks_per_pair;
-  hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(CNT), 0, s, a,
+  hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)(blocks < MOST_GROUPS ? blocks : MOST_GROUPS)), dim3(CNT), 0, s, a,
                      src, dst);
   return hipGetLastError();
 }
@@ -471,7 +474,7 @@ hipError_t launch_pages_extend(hipStream_t s, const PageMap &m, const int32_t *n
 
 hipError_t launch_pages_free(hipStream_t s, const PageMap &m, int n, const int32_t *seqs) {
   if (n <= 0) return hipSuccess;
-  hipLaunchKernelGGL(free_kernel, dim3(n), dim3(CNT), 0, s, m, seqs);
+  hipLaunchKernelGGL(free_kernel, dim3(n < MOST_GROUPS ? n : MOST_GROUPS), dim3(CNT), 0, s, m, n, seqs);
   return hipGetLastError();
 }
 

@@ -99,7 +99,7 @@ class Server:
 
     def free(self, seqs):
         flags = 0
-        for s in seqs:
+        for s in dict.fromkeys(seqs):
             if not 0 <= s < len(self.lengths):
                 flags |= 2
                 continue
@@ -260,3 +260,12 @@ def test_map_limits():
     s.upload()
     s.compact()
     s.free(list(range(4096)))
+
+
+def test_a_list_longer_than_a_launch():
+    """More names than workgroups that a launch may have: each sequence is freed, the last one named at the end alone."""
+    print("[case] long list", flush=True)
+    s = Server(64, 12, 8)
+    s.extend([5] * 12)
+    s.free([i % 11 for i in range((1 << 24) + 3)] + [11])
+    assert s.refs == [0] * 64

@@ -123,6 +123,35 @@ def test_far_positions_and_many_rows():
         assert ctx.device_errors() == 0
 
 
+def test_more_rows_than_a_launch_takes():
+    """Tokens behind four million rows of nobody are appended as if alone."""
+    import paper_2609_30884_amd as crf
+    from tests.paged import Batch, context
+    print("[case] rope behind 2^22 rows", flush=True)
+    b = Batch([(3, 20)], 2, 2, 64, torch.bfloat16, seed=3)
+    ctx, plan, far = context(2, 2, 64, torch.bfloat16), crf.rope(64, 1e4), (1 << 22) + 9
+    x = torch.zeros(far + 3, 6, 64, dtype=torch.bfloat16, device="cuda")
+    x[far:] = torch.randn(3, 6, 64, device="cuda")
+    some = [x[:, 2 * i:2 * i + 2] for i in range(3)]
+    outs, pools = [], []
+    for first in (far, 0):
+        t = [y[far - first:] for y in some]
+        batch = crf.seq_batch(b.row_start + first, b.length, b.tables, first + 3, 3)
+        out = torch.zeros(first + 3, 2, 64, dtype=torch.bfloat16, device="cuda")
+        crf.rope_append(ctx, plan, batch, *t, b.pool, 1, out)
+        torch.cuda.synchronize()
+        assert (out[:first] == 0).all() and out[first:].any()
+        outs.append(out[first:].clone())
+        pools.append([b.k_pool.clone(), b.v_pool.clone()])
+        b.k_pool.zero_()
+        b.v_pool.zero_()
+    pg, sl = b.places(0, torch.tensor([20, 21, 22]))
+    assert torch.equal(outs[0], outs[1])
+    for p, q in zip(*pools):
+        assert torch.equal(p[1, pg, :, sl], q[1, pg, :, sl]) and q[1, pg, :, sl].any()
+    assert ctx.device_errors() == 0
+
+
 def test_in_place_and_pages_out_of_range():
     import paper_2609_30884_amd as crf
     from tests.paged import Batch, context

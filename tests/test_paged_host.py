@@ -113,3 +113,9 @@ def test_rope_plans():
                  dict(scaling="linear", factor=0.0), dict(scaling="parts", factor=2.0)):
         with pytest.raises(crf.CrfError):
             crf.rope(**{**dict(rotary_dim=64, theta=1e4), **args})
+
+
+def test_rope_plans_are_finite():
+    for args in (dict(theta=1e-320), dict(scaling="base", factor=1e-320), dict(mscale=1e300), dict(mscale=float("nan"))):
+        with pytest.raises(crf.CrfError):
+            crf.rope(**{**dict(rotary_dim=128, theta=1e4), **args})
