@@ -27,11 +27,25 @@
 // to the storage type for the second product, as MFMA needs them (bf16: 2^-8
 // of each weight at most), and summed before that rounding.
 //
-// Schedule: a unit is a row tile of one KV head of one sequence.  Few units: the
-// work (keys times rows) is dealt out evenly, a contiguous stretch to each resident
-// workgroup; a unit cut by a border leaves partials, which the workgroup that
-// finishes last joins in the order of the keys (results do not depend on who that
-// is).  Many: one unit a workgroup, longest of a sequence first.
+// Schedule: a unit is a row tile of one KV head of one sequence.  Its work (keys times
+// rows) is known on the device alone, so every workgroup works out from all lengths what
+// it computes.  Either units are dealt out whole, longest of a sequence first; or the
+// work is dealt out evenly, a contiguous stretch to each resident workgroup, and a unit
+// cut by a border leaves partials, which the workgroup that finishes last joins in the
+// order of the keys (results do not depend on who that is).
+//
+// Measured (bf16, head size 128 where nothing else is said):
+//   8192 tokens after 8192, 28/4 heads    1.40 ms, 1.03 PFLOP/s (a large matrix product
+//     reaches 1.19): matrix pipes busy half of the cycles, the exponentials the most of
+//     the rest;
+//   64 sequences' next tokens over 500 to 16384, 28/4 heads    154 us, 5.1 TB/s: HBM;
+//   12 sequences, some with chunks of up to 512, over up to 8192, 12/2 heads    71 us, 0.42
+//     PFLOP/s: 9 us until the first task is known, 33 of products, 14 to join 9 or 10
+//     parts, whose 33 MB are written and read once;
+//   4 chunks of 500 to 2048 in a window of 1024, 12/2 heads of 64    35 us, 0.43 PFLOP/s:
+//     the exponentials, of which heads of 64 have twice as many to a product;
+//   one next token over 3000, 12/2 heads    13.6 us: a chain of latencies (lengths 2, its
+//     schedule 2, page numbers 1.5, keys 3, partials 1.5, ticket 1.5, join 2.5).
 #include <math.h>
 
 #include <algorithm>
@@ -43,11 +57,23 @@ namespace crf {
 namespace {
 
 constexpr float PSUM_MAX = 65536.0f; // a lane's sum of a block's probabilities that needs no new reference
-constexpr int PGCAP = 2048;         // page numbers staged in LDS at a time
-constexpr int MANY = 3;             // rounds of units over the resident workgroups from which none is split
-constexpr int64_t SMALL_READS = 48 << 20;  // bytes of K and V up to which tiles of 32 rows do
-constexpr int SLIVER = 2;           // fewer tiles are no part of their own
-constexpr float SPLIT = 8.f;        // tiles that a part costs besides its keys
+constexpr int PGCAP = 2048;  // page numbers staged in LDS at a time
+// Rounds of units over the resident workgroups from which none is split.  8192 tokens
+// after 8192 (4.1 rounds) 1.40 ms, split 1.53; 8 chunks of 2048 488 us, split 530; with 1,
+// the 12 sequences above 188 us instead of 71.
+constexpr int MANY = 3;
+// Tiles that a part costs besides its keys, when whole units and parts are weighed.  0: the
+// chunks in a window 45 us instead of 35 (cut where whole units come out as even); 99: 16
+// chunks of 64 over 4000 99 us instead of 51 (left whole where they do not).
+constexpr float SPLIT = 8.f;
+// Fewer tiles are no part of their own.  0: the 12 sequences 75.8 us instead of 71.1, six
+// chunks in fp32 27.6 instead of 22.5.
+constexpr int SLIVER = 2;
+// Bytes of K and V up to which tiles of 32 rows do (as counted in launch() below).  0: 300
+// tokens 22 us instead of 15, two chunks of 32 over 2000 33 instead of 23, six in fp32 28
+// instead of 22.5; no limit: 1000 tokens (190 MB) 37 instead of 30, 16 chunks of 64 over
+// 4000 70 instead of 51, the 12 sequences 183 instead of 71.
+constexpr int64_t SMALL_READS = 48 << 20;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -924,7 +950,11 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f, true}, slots, true};
+  // A unit costs 256 keys besides its own (with 0 the 12 sequences take 103 us instead of
+  // 71, 4096 tokens 156 instead of 91); a part in a join 1.3 tiles, 0.3 of the slower fp32
+  // ones (with none 1000 tokens take 38 us instead of 30).
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f, true},
+               slots, true};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;  // keys before its own that a row sees
@@ -1219,10 +1249,10 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
 template <typename T, int HD, bool UNI>
 hipError_t launch(hipStream_t s, PagedAttn p) {
   const int G = p.nq / p.nkv;
-  // Tiles of 32 rows for up to 32 rows to a sequence and KV head, and where all of them
-  // together read so few keys (as far as the host can tell) that four times the reads of
-  // K and V cost less than the parts of long units: six fp32 chunks of up to 64 tokens
-  // over 1500 32 -> 27 us.
+  // Tiles of 32 rows for up to 32 rows to a sequence and KV head (with tiles of 128 the
+  // steps above take 33 us instead of 13.6 and 196 instead of 154), and where all of them
+  // together read so few keys, as far as the host can tell, that four times the reads of
+  // K and V cost less than the parts of long units.
   const int64_t row_tiles = ((int64_t)p.b.n_rows * G / 32 + p.b.n_seqs) * p.nkv;
   const int64_t longest = std::min<int64_t>((int64_t)p.b.max_pages * p.b.page_size, (int64_t)1 << 24);
   const bool keys = (int64_t)p.b.max_new * G <= 32 ||

@@ -6,7 +6,12 @@
 // of the sequences that need them.  A plan is made by one workgroup, which holds
 // one bit per page in LDS (bit set: the page is in use), counts the bits of a
 // run of words per thread and scans the counts; the pages' bytes are moved by a
-// launch of its own over all compute units.  Moving the bytes is HBM bound.
+// launch of its own over all compute units.
+//
+// Moving the bytes is HBM bound: a compaction of 5500 pages of 28 layers, bf16, moves 651
+// MB in 138 us, 4.7 TB/s (a large copy reaches 5.0).  The plans are latency: one
+// workgroup, a chain of loads, a scan and stores (fork 5.1 us, extend 5.1, compact 7.8,
+// free 3.3); more workgroups would have to agree on the order of the free pages.
 #include "paged.hpp"
 
 namespace crf {
@@ -99,7 +104,7 @@ CRF_DEV void load_bits(const int32_t *refs, int n_pages, uint64_t *bits, bool pa
 // ---------------------------------------------------------------- copying
 
 // Chunks of 16 bytes: pair i holds 2 pools x layers x cpp of them.  A thread takes
-// CUN of a pair's chunks, NT apart, all loads in flight before the first store.
+// CUN of a pair's chunks, CNT apart, all loads in flight before the first store.
 constexpr int CNT = 256, CUN = 8;
 
 struct CopyArgs {
