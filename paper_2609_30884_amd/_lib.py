@@ -421,8 +421,9 @@ def _int32(t, n: Optional[int], name: str):
 
 def _tables(t):
     import torch
-    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise CrfError(2, "block tables must be int32 [sequences, entries], entries contiguous")
+    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or \
+            (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise CrfError(2, "block tables must be int32 [sequences, entries], entries contiguous, rows that do not overlap")
     return t
 
 
@@ -449,7 +450,7 @@ def _head_rows(d: ModelDims, t, n_rows: int, heads: int, name: str):
 def page_pool(k_pool, v_pool, page_size: int) -> PagePool:
     """k_pool, v_pool: [n_layers, n_pages, n_kv_heads, page_size, head_dim] device tensors."""
     if k_pool.dtype is not v_pool.dtype or k_pool.shape != v_pool.shape or k_pool.stride() != v_pool.stride() or \
-            k_pool.dim() != 5 or not k_pool[0, 0].is_contiguous() or k_pool.shape[3] != page_size:
+            k_pool.dim() != 5 or (k_pool.numel() and not k_pool[0, 0].is_contiguous()) or k_pool.shape[3] != page_size:
         raise CrfError(2, "pools must be two like tensors [layers, pages, kv heads, page_size, head_dim], pages contiguous")
     p = PagePool(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), k_pool.stride(1), k_pool.shape[1], page_size)
     p.tensors, p.device = (k_pool, v_pool), _same_device(k_pool, v_pool)
@@ -472,7 +473,7 @@ def seq_batch(row_start, length, block_tables, n_rows: int, max_new: int = 0) ->
     calls' tensors; max_new: the most new tokens of a sequence (0: n_rows)."""
     t = _tables(block_tables)
     n = t.shape[0]
-    b = SeqBatch(n, int(n_rows), int(max_new), t.shape[1], max(t.stride(0), t.shape[1]) if n > 1 else t.shape[1],
+    b = SeqBatch(n, int(n_rows), int(max_new), t.shape[1], t.stride(0) if n > 1 else t.shape[1],
                  _int32(row_start, n + 1, "row_start").data_ptr(), _int32(length, n, "length").data_ptr(), t.data_ptr())
     b.tensors, b.device = (row_start, length, block_tables), _same_device(row_start, length, block_tables)
     return b
@@ -541,7 +542,7 @@ def page_map(refs, block_tables, lengths, page_size: int) -> PageMap:
     t = _tables(block_tables)
     n = t.shape[0]
     m = PageMap(_int32(refs, None, "refs").data_ptr(), t.data_ptr(), _int32(lengths, n, "lengths").data_ptr(),
-                max(t.stride(0), t.shape[1]) if n > 1 else t.shape[1], refs.numel(), int(page_size), n, t.shape[1])
+                t.stride(0) if n > 1 else t.shape[1], refs.numel(), int(page_size), n, t.shape[1])
     m.tensors, m.device = (refs, block_tables, lengths), _same_device(refs, block_tables, lengths)
     return m
 

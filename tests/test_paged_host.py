@@ -119,3 +119,16 @@ def test_rope_plans_are_finite():
     for args in (dict(theta=1e-320), dict(scaling="base", factor=1e-320), dict(mscale=1e300), dict(mscale=float("nan"))):
         with pytest.raises(crf.CrfError):
             crf.rope(**{**dict(rotary_dim=128, theta=1e4), **args})
+
+
+def test_tables_whose_rows_overlap():
+    """One table for several sequences is no table of several rows: its stride would read past it."""
+    one = _i32(1, 5)
+    with pytest.raises(crf.CrfError):
+        crf.seq_batch(_i32(4), _i32(3), one.expand(3, 5), 3)
+    with pytest.raises(crf.CrfError):
+        crf.page_map(_i32(8), torch.as_strided(_i32(9), (3, 5), (2, 1)), _i32(3), 16)
+    assert crf.seq_batch(_i32(2), _i32(1), one.expand(1, 5), 3).table_stride == 5
+    assert crf.page_map(_i32(8), _i32(3, 9)[:, :5], _i32(3), 16).table_stride == 9
+    empty = torch.zeros(2, 0, 2, 16, 64, dtype=torch.bfloat16)
+    assert crf.page_pool(empty, empty, 16).n_pages == 0
