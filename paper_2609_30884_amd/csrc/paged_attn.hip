@@ -158,6 +158,12 @@ struct QFrag {
 #pragma unroll
     for (int s = 0; s < Layout<T, HD>::KS; ++s) f[s] = ld16(row + (2 * s + g) * Layout<T, HD>::EPC);
   }
+  // The row has arrived.  (Else the compiler, which does not count the loads to LDS, waits
+  // inside the loop over the keys for what it takes for these loads: for the next tile.)
+  CRF_DEV void arrived() {
+#pragma unroll
+    for (int s = 0; s < Layout<T, HD>::KS; ++s) asm volatile("" : "+v"(f[s]));
+  }
 };
 
 // The keys that a lane's row sees: [lo, hi]; bad: some pages of the unit are out of
@@ -1006,6 +1012,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
           load(it + 1, (it + 1 - t.t0) & 1);
         }
       };
+      q.arrived();
 #pragma unroll 1
       for (int it = t.t0; it < t.t1;) {
         // tiles that every row of the wave sees; the first block of all gives the rows
@@ -1155,6 +1162,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         };
         load(a);
         if (a + 1 < z) load(a + 1);
+        q.arrived();
 #pragma unroll 1
         for (int it = a; it < z;) {
           for (;;) {
