@@ -329,6 +329,51 @@ CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, in
   }
 }
 
+// O += P V for NB blocks in bf16, whose V fragments are read two groups of products ahead
+// (a group: two products, of the 32 rows b of O^T); ahead() reads the first two.
+template <int HD, int NB>
+struct Weigh {
+  using L = Layout<bf16, HD>;
+  static constexpr int GROUPS = NB * L::HB;
+  const lds_mem *vt;
+  uint32_t va;
+  s16x4 x[3][4];
+
+  CRF_DEV void read(int i) {
+    const lds_mem *v = vt + 32 * (i / L::HB) * L::ROWB;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[i % 3][r] = lds_tr(v + 8 * r * L::ROWB + (va ^ (64 * (i % L::HB))));
+  }
+  CRF_DEV void ahead(const lds_mem *v, int lane) {
+    vt = v;
+    va = L::vaddr(lane);
+    fresh(va);
+    read(0);
+    read(1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  CRF_DEV void add(const float (&p)[NB][16], RowState<HD> &st) {
+    bf16x8 pf[2];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      if (i % L::HB == 0)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[h][e] = f2bf(p[i / L::HB][8 * h + e]);
+      if (i + 2 < GROUPS) read(i + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 &o = st.o[i % L::HB];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s16x4 f[2] = {x[i % 3][2 * h], x[i % 3][2 * h + 1]};
+        o = mfma32(__builtin_bit_cast(bf16x8, f), pf[h], o);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
 // NB blocks of 32 keys that every row sees.  False, with nothing
 // changed, if some row needs another reference: then the blocks are taken one by one
 // as below (the code that rescales O stays out of the loop over the others).
@@ -337,6 +382,8 @@ CRF_DEV bool whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, H
                           int lane) {
   f32x16 s[NB];
   scores<T, HD, NB>(kt, q, lane, s);
+  Weigh<HD, NB> w;
+  if constexpr (sizeof(T) == 2) w.ahead(vt, lane);
   float p[NB][16], sum[NB];
   bool raise = false;
 #pragma unroll
@@ -351,10 +398,12 @@ CRF_DEV bool whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, H
   }
   if (__builtin_amdgcn_ballot_w64(raise)) return false;
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb) {
-    st.l += sum[kb];
-    weigh<T, HD, ALL>(vt + 32 * kb * Layout<T, HD>::ROWB, p[kb], st, lane);
-  }
+  for (int kb = 0; kb < NB; ++kb) st.l += sum[kb];
+  if constexpr (sizeof(T) == 2)
+    w.add(p, st);
+  else
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) weigh<T, HD, ALL>(vt + 32 * kb * Layout<T, HD>::ROWB, p[kb], st, lane);
   return true;
 }
 
