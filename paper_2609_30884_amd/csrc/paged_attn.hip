@@ -98,13 +98,30 @@ CRF_DEV u32x4 resource(const void *base, uint32_t bytes) {
   const uint64_t a = (uint64_t)base;
   return u32x4{scalar((uint32_t)a), scalar((uint32_t)(a >> 32) & 0xffffu), scalar(bytes), 0x00020000u};
 }
-CRF_DEV void dma_page(u32x4 kr, u32x4 vr, const lds_mem *kl, const lds_mem *vl, uint32_t ko, uint32_t vo) {
-  asm volatile(
-      "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
-      "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds"
-      :
-      : "s"(scalar((uint32_t)(uintptr_t)kl)), "s"(scalar((uint32_t)(uintptr_t)vl)), "v"(ko), "v"(vo), "s"(kr), "s"(vr)
-      : "memory");
+// N x 1 KiB of K and of V, load i's at i KiB: the instruction's offset counts in both addresses.
+template <int N>
+CRF_DEV void dma_page(u32x4 kr, u32x4 vr, const lds_mem *kl, const lds_mem *vl, const uint32_t (&ko)[4], uint32_t vo) {
+  const uint32_t k = scalar((uint32_t)(uintptr_t)kl), v = scalar((uint32_t)(uintptr_t)vl);
+  if constexpr (N == 4)
+    asm volatile(
+        "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %7, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %3, %7, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %4, %7, 0 offen offset:2048 lds\n\t"
+        "buffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %8, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %6, %8, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %6, %8, 0 offen offset:2048 lds\n\t"
+        "buffer_load_dwordx4 %6, %8, 0 offen offset:3072 lds"
+        :
+        : "s"(k), "s"(v), "v"(ko[0]), "v"(ko[1]), "v"(ko[2]), "v"(ko[3]), "v"(vo), "s"(kr), "s"(vr)
+        : "memory");
+  else
+    asm volatile(
+        "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %3, %5, 0 offen offset:1024 lds\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %6, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %4, %6, 0 offen offset:1024 lds"
+        :
+        : "s"(k), "s"(v), "v"(ko[0]), "v"(ko[1]), "v"(vo), "s"(kr), "s"(vr)
+        : "memory");
 }
 // Rows of their own: an address a lane.
 CRF_DEV void dma_row(const char *k, const char *v, const lds_mem *kl, const lds_mem *vl) {
@@ -972,9 +989,15 @@ struct Pages {
             q < 0 ? 0 : q * b.page_bytes + (int64_t)(kvh * b.page_size + kg - lp * b.page_size) * L::ROWB;
         const uint32_t bytes = q < 0 ? 0 : rows * L::ROWB;
         const u32x4 kr = resource(b.k + off, bytes), vr = resource(b.v + off, bytes);
+        constexpr int LOADS = GRP / L::RPI, N = LOADS < 4 ? LOADS : 4;
+        static_assert(LOADS == 2 || LOADS % 4 == 0, "loads of a group");
 #pragma unroll
-        for (int i = 0; i < GRP / L::RPI; ++i)
-          dma_page(kr, vr, kl + i * 1024, vl + i * 1024, kbytes(i, k0) + i * 1024, v0 + i * 1024);
+        for (int i = 0; i < LOADS; i += N) {
+          uint32_t k[4];
+#pragma unroll
+          for (int j = 0; j < N; ++j) k[j] = kbytes(i + j, k0) + i * 1024;
+          dma_page<N>(kr, vr, kl + i * 1024, vl + i * 1024, k, v0 + i * 1024);
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < GRP / L::RPI; ++i) {
