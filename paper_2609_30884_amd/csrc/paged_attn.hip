@@ -35,11 +35,11 @@
 // order of the keys (results do not depend on who that is).
 //
 // Measured (bf16, head size 128 where nothing else is said):
-//   8192 tokens after 8192, 28/4 heads    1.40 ms, 1.03 PFLOP/s (a large matrix product
-//     reaches 1.19): matrix pipes busy half of the cycles, the exponentials the most of
-//     the rest;
-//   64 sequences' next tokens over 500 to 16384, 28/4 heads    154 us, 5.1 TB/s: HBM;
-//   12 sequences, some with chunks of up to 512, over up to 8192, 12/2 heads    71 us, 0.42
+//   8192 tokens after 8192, 28/4 heads    1.38 ms, 1.04 PFLOP/s (a large matrix product
+//     reaches 1.19).  Matrix pipes are busy half of the cycles; without the exponentials
+//     it would take 1.20 ms, without the loads to LDS as much, without both 1.05;
+//   64 sequences' next tokens over 500 to 16384, 28/4 heads    152 us, 5.2 TB/s: HBM;
+//   12 sequences, some with chunks of up to 512, over up to 8192, 12/2 heads    70 us, 0.43
 //     PFLOP/s: 9 us until the first task is known, 33 of products, 14 to join 9 or 10
 //     parts, whose 33 MB are written and read once;
 //   4 chunks of 500 to 2048 in a window of 1024, 12/2 heads of 64    35 us, 0.43 PFLOP/s:
