@@ -19,7 +19,8 @@ constexpr int PAGED_ZERO_BYTES = 1024;
 constexpr int PAGED_MAX_LIST = 4096;   // forks of a call; sequences of a page map
 constexpr int PAGED_MAX_PAGES = 1 << 19;  // pages of a page map
 constexpr int PAGED_TICKETS = 1024;
-constexpr int MOST_GROUPS = 1 << 20;   // workgroups of a launch (a grid holds fewer than 2^32 threads); the kernels loop
+// Workgroups of a launch (a grid holds fewer than 2^32 threads); past them the kernels loop.
+constexpr int MOST_GROUPS = 1 << 20;
 constexpr size_t PAGED_WS_BYTES = PAGED_ZERO_BYTES + sizeof(int) * (PAGED_MAX_LIST + PAGED_TICKETS);
 constexpr int64_t PAGED_PART_FLOATS = (int64_t)1 << 24;  // fp32 contexts: 64 MiB of attention partials
 

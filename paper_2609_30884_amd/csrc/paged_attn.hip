@@ -105,20 +105,20 @@ CRF_DEV void dma_page(u32x4 kr, u32x4 vr, const lds_mem *kl, const lds_mem *vl, 
   if constexpr (N == 4)
     asm volatile(
         "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %7, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %3, %7, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %4, %7, 0 offen offset:2048 lds\n\t"
-        "buffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds\n\t"
+        "buffer_load_dwordx4 %3, %7, 0 offen offset:0x400 lds\n\tbuffer_load_dwordx4 %4, %7, 0 offen offset:0x800 lds\n\t"
+        "buffer_load_dwordx4 %5, %7, 0 offen offset:0xc00 lds\n\t"
         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %8, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %6, %8, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %6, %8, 0 offen offset:2048 lds\n\t"
-        "buffer_load_dwordx4 %6, %8, 0 offen offset:3072 lds"
+        "buffer_load_dwordx4 %6, %8, 0 offen offset:0x400 lds\n\tbuffer_load_dwordx4 %6, %8, 0 offen offset:0x800 lds\n\t"
+        "buffer_load_dwordx4 %6, %8, 0 offen offset:0xc00 lds"
         :
         : "s"(k), "s"(v), "v"(ko[0]), "v"(ko[1]), "v"(ko[2]), "v"(ko[3]), "v"(vo), "s"(kr), "s"(vr)
         : "memory");
   else
     asm volatile(
         "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %3, %5, 0 offen offset:1024 lds\n\t"
+        "buffer_load_dwordx4 %3, %5, 0 offen offset:0x400 lds\n\t"
         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %6, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %4, %6, 0 offen offset:1024 lds"
+        "buffer_load_dwordx4 %4, %6, 0 offen offset:0x400 lds"
         :
         : "s"(k), "s"(v), "v"(ko[0]), "v"(ko[1]), "v"(vo), "s"(kr), "s"(vr)
         : "memory");
@@ -801,11 +801,13 @@ struct Schedule {
       if (many) {
         Lane q;
         pass(at, true, q);
+        if (__builtin_amdgcn_readfirstlane(!(at >= base && at < base + work))) return false;
       } else {
 #pragma unroll 1
         while (__builtin_amdgcn_readfirstlane(at >= base + work)) {  // (some sequence holds `at`)
           base += work;
-          n = seq_new(p.b, ++seq, start, len);
+          if (++seq >= p.b.n_seqs) return false;
+          n = seq_new(p.b, seq, start, len);
           work = n > 0 ? sh.seq_work(n, len) : 0;
         }
       }
@@ -953,7 +955,9 @@ struct Pages {
   const int32_t *table;
 
   // A lane's bytes from the first of the rows that load i of a group covers (1 KiB).
-  CRF_DEV uint32_t kbytes(int i, uint32_t k0) const { return k0 ^ (((i * L::RPI) & (L::CH < 16 ? L::CH - 1 : 15)) * 16); }
+  CRF_DEV uint32_t kbytes(int i, uint32_t k0) const {
+    return k0 ^ (((i * L::RPI) & (L::CH < 16 ? L::CH - 1 : 15)) * 16);
+  }
   // (V's slots repeat every 4 rows: RPI is a multiple of that wherever it has any)
   static_assert(sizeof(T) == 4 || L::RPI % 4 == 0, "V rows of a load");
 
@@ -1009,7 +1013,8 @@ struct Pages {
             slot = key - lp * b.page_size;
           }
           const int64_t o = q * b.page_bytes + (int64_t)(kvh * b.page_size + slot - lrow) * L::ROWB;
-          dma_row(q >= 0 ? b.k + o + kbytes(i, k0) : zeros, q >= 0 ? b.v + o + v0 : zeros, kl + i * 1024, vl + i * 1024);
+          dma_row(q >= 0 ? b.k + o + kbytes(i, k0) : zeros, q >= 0 ? b.v + o + v0 : zeros, kl + i * 1024,
+                  vl + i * 1024);
         }
       }
     }
@@ -1100,14 +1105,17 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         if (it == t.t1) break;
         const int kt0 = it * BKV;
         if (wave * 32 < rows && kt0 <= pos_hi && kt0 + BKV > first_seen) {
-          const Seen seen{pos > far ? pos - far : 0, pos, last_first, whole_to, t.len, bad != 0, pg, pages.first, p.b.ps_div};
+          const Seen seen{pos > far ? pos - far : 0, pos,         last_first, whole_to, t.len, bad != 0, pg,
+                          pages.first,               p.b.ps_div};
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
 #pragma unroll 1
           for (int kb = 0; kb < BKV; kb += 32)
             if (careful)
-              block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane, seen);
+              block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
+                                    seen);
             else
-              block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane, seen);
+              block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
+                                 seen);
         }
         ++it;
       }
