@@ -36,8 +36,8 @@
 //
 // Measured (bf16, head size 128 where nothing else is said):
 //   8192 tokens after 8192, 28/4 heads    1.38 ms, 1.04 PFLOP/s (a large matrix product
-//     reaches 1.19).  Matrix pipes are busy half of the cycles; without the exponentials
-//     it would take 1.20 ms, without the loads to LDS as much, without both 1.05;
+//     reaches 1.19).  Matrix pipes are busy half of the cycles; with all exponentials of
+//     a tile before its second product, 1.42;
 //   64 sequences' next tokens over 500 to 16384, 28/4 heads    152 us, 5.2 TB/s: HBM;
 //   12 sequences, some with chunks of up to 512, over up to 8192, 12/2 heads    70 us, 0.43
 //     PFLOP/s: 9 us until the first task is known, 33 of products, 14 to join 9 or 10
@@ -373,59 +373,79 @@ struct Weigh {
     read(1);
     __builtin_amdgcn_sched_barrier(0);
   }
-  CRF_DEV void add(const float (&p)[NB][16], RowState<HD> &st) {
+  // Block KB; during(j) is vector work for behind the j-th of its 2 HB products.
+  template <int KB, typename F>
+  CRF_DEV void add(const float (&p)[16], RowState<HD> &st, F during) {
     bf16x8 pf[2];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      if (i % L::HB == 0)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int e = 0; e < 8; ++e) pf[h][e] = f2bf(p[8 * h + e]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pf[h][e] = f2bf(p[i / L::HB][8 * h + e]);
+    for (int b = 0; b < L::HB; ++b) {
+      const int i = KB * L::HB + b;
       if (i + 2 < GROUPS) read(i + 2);
       __builtin_amdgcn_sched_barrier(0);
-      f32x16 &o = st.o[i % L::HB];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         s16x4 f[2] = {x[i % 3][2 * h], x[i % 3][2 * h + 1]};
-        o = mfma32(__builtin_bit_cast(bf16x8, f), pf[h], o);
+        st.o[b] = mfma32(__builtin_bit_cast(bf16x8, f), pf[h], st.o[b]);
+        during(2 * b + h);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
   }
 };
 
-// NB blocks of 32 keys that every row sees.  False, with nothing
-// changed, if some row needs another reference: then the blocks are taken one by one
-// as below (the code that rescales O stays out of the loop over the others).
+// Up to NB blocks of 32 keys that every row sees; returns how many it has taken.  The
+// next one needs another reference for some row, and is taken as below (the code that
+// rescales O stays out of the loop over the others).  In bf16 a block's exponentials are
+// formed between the products of the one before.
 template <typename T, int HD, int NB>
-CRF_DEV bool whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, HD> &q, RowState<HD> &st, float c,
-                          int lane) {
+CRF_DEV int whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, HD> &q, RowState<HD> &st, float c,
+                         int lane) {
   f32x16 s[NB];
   scores<T, HD, NB>(kt, q, lane, s);
-  Weigh<HD, NB> w;
-  if constexpr (sizeof(T) == 2) w.ahead(vt, lane);
   float p[NB][16], sum[NB];
-  bool raise = false;
+  auto weights = [&](int kb, int v0, int v1) {
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb) {
-    sum[kb] = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
+    for (int v = v0; v < v1; ++v) {
       p[kb][v] = fast_exp2(fmaf(s[kb][v], c, -st.ref));
-      sum[kb] += p[kb][v];
+      sum[kb] = v == 0 ? p[kb][v] : sum[kb] + p[kb][v];
     }
-    raise |= !(sum[kb] <= PSUM_MAX);  // (also where the sum is no number)
+  };
+  auto raised = [&](int kb) {  // (also where the sum is no number)
+    return __builtin_amdgcn_ballot_w64(!(sum[kb] <= PSUM_MAX)) != 0;
+  };
+  if constexpr (sizeof(T) == 2) {
+    static_assert(NB <= 2, "blocks");
+    constexpr int EACH = 16 / (2 * Layout<T, HD>::HB);
+    Weigh<HD, NB> w;
+    w.ahead(vt, lane);
+    weights(0, 0, 16);
+    if (raised(0)) return 0;
+    st.l += sum[0];
+    w.template add<0>(p[0], st, [&](int j) {
+      if (NB > 1) weights(NB - 1, EACH * j, EACH * (j + 1));
+    });
+    if (NB > 1) {
+      if (raised(NB - 1)) return 1;
+      st.l += sum[NB - 1];
+      w.template add<NB - 1>(p[NB - 1], st, [](int) {});
+    }
+  } else {
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) weights(kb, 0, 16);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+      if (raised(kb)) return 0;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      st.l += sum[kb];
+      weigh<T, HD, ALL>(vt + 32 * kb * Layout<T, HD>::ROWB, p[kb], st, lane);
+    }
   }
-  if (__builtin_amdgcn_ballot_w64(raise)) return false;
-#pragma unroll
-  for (int kb = 0; kb < NB; ++kb) st.l += sum[kb];
-  if constexpr (sizeof(T) == 2)
-    w.add(p, st);
-  else
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) weigh<T, HD, ALL>(vt + 32 * kb * Layout<T, HD>::ROWB, p[kb], st, lane);
-  return true;
+  return NB;
 }
 
 // One block of 32 keys, key0 ..: scores, probabilities, O += P V.
@@ -1098,12 +1118,15 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
       for (int it = t.t0; it < t.t1;) {
         // tiles that every row of the wave sees; the first block of all gives the rows
         // their reference
+        int taken = 0;  // blocks of the tile
         for (;;) {
           arrive(it);
           const int kt0 = it * BKV;
           if (it == t.t0 || kt0 + BKV > whole_to || kt0 < last_first || bad || careful) break;
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
-          if (!whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
+          taken = whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane);
+          if (taken < BKV / 32) break;
+          taken = 0;
           if (++it == t.t1) break;
         }
         if (it == t.t1) break;
@@ -1113,7 +1136,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
                           pages.first,               p.b.ps_div};
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
 #pragma unroll 1
-          for (int kb = 0; kb < BKV; kb += 32)
+          for (int kb = 32 * taken; kb < BKV; kb += 32)
             if (careful)
               block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
                                     seen);

@@ -126,6 +126,22 @@ def test_scale_and_strides(dtype):
     assert torch.equal(b.q.reshape(b.n_rows, 256), out[:, :256])
 
 
+@pytest.mark.parametrize("dtype,hd,nq,seqs", [
+    (BF, 128, 12, [(60, 1500), (200, 700)]), (BF, 64, 12, [(130, 900), (64, 333)]), (F32, 64, 4, [(150, 700)]),
+    (F32, 128, 4, [(130, 400)]), (BF, 128, 12, [(1, 1500), (2, 900), (1, 40)]), (F32, 64, 4, [(1, 1500), (3, 200)])])
+def test_keys_that_outweigh_all_before(dtype, hd, nq, seqs):
+    """A few keys score 40 times the others, in the first and the second half of tiles of 64 and of 128: the reference
+    rises in the middle of a prefix, for some rows of a tile and not for others, or falls behind at once."""
+    from tests.paged import Batch
+    print(f"[case] spikes {dtype} hd {hd} {seqs}", flush=True)
+    b = Batch(seqs, nq, 2, hd, _dt(dtype), seed=23)
+    for s, t in enumerate(b.total):
+        spikes = (3, 37, 70, 101, 135, 200, 230, 290, 355, 420, 500, 707, 1100)
+        pg, sl = b.places(s, torch.tensor([x for x in spikes if x < t]))
+        b.k_pool[1, pg, :, sl] *= 40
+    _check(b, "spikes")
+
+
 @pytest.mark.parametrize("dtype,hd,seqs", [(BF, 128, [(40, 2000), (100, 900)]), (BF, 64, [(1, 2000), (2, 500)]),
                                            (F32, 64, [(90, 1500)])])
 def test_values_near_the_largest(dtype, hd, seqs):
