@@ -1146,7 +1146,9 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         }
         ++it;
       }
-      if (careful || !__syncthreads_or(!st.finite())) break;
+      // (a barrier after every pass: the next task clears `bad`, which the last tile reads)
+      const bool again = __syncthreads_or(!st.finite());
+      if (careful || !again) break;
       careful = true;
     }
 
