@@ -197,6 +197,7 @@ struct Seen {
   const int *pages;  // staged page numbers, the first of logical page `first`
   int first;
   FastDiv ps_div;
+  uint64_t strict;  // CAREFUL: lanes whose reference is the maximum
   CRF_DEV bool all(int key0) const { return key0 >= all_from && key0 + 32 <= all_to; }
 };
 
@@ -204,7 +205,7 @@ template <int HD>
 struct RowState {
   f32x16 o[HD / 32];
   float ref, l;
-  CRF_DEV bool finite() const {
+  CRF_DEV bool finite() const {  // (what the lane holds of its row)
     float z = 0.f;
 #pragma unroll
     for (int b = 0; b < HD / 32; ++b)
@@ -262,10 +263,22 @@ CRF_DEV void scores(const lds_mem *kt, const QFrag<T, HD> &q, int lane, f32x16 (
 // SOME: some row does not see some key, or needs another reference.  CAREFUL: a value
 // that is not finite may belong to a key that some row does not see: the product would
 // multiply it by that row's weight zero, so such values are taken out of the product and
-// added where the weight is not zero; and the reference is the maximum, so that large
-// values times weights of up to PSUM_MAX stay in range.  (Units run without it first,
-// and again if their result is not finite.)
+// added where the weight is not zero.
+//
+// A unit runs without it first, and again with it if some row's result is not finite; the
+// references are raised as before, so that a row that saw none of those values keeps every
+// bit.  A third run is for rows that still are not: their reference is the maximum (STRICT),
+// as large values times weights of up to PSUM_MAX may have passed the range.  Which rows
+// those are depends on what they see alone.
 enum Take { ALL, SOME, CAREFUL };
+constexpr float STRICT = 16.f;  // a lane's 16 weights of up to 1
+
+// The lanes of the rows that are not finite; a row's two lanes agree.
+template <int HD>
+CRF_DEV uint64_t not_finite(const RowState<HD> &st) {
+  const uint64_t m = __builtin_amdgcn_ballot_w64(!st.finite());
+  return m | m >> 32 | m << 32;
+}
 
 // O += P V for the probabilities p of 32 keys (V rows from vt on).
 template <typename T, int HD, Take TAKE>
@@ -452,7 +465,7 @@ CRF_DEV int whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, HD
 template <typename T, int HD, Take TAKE>
 CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
                    int lane, const Seen &seen) {
-  constexpr float most = TAKE == CAREFUL ? 16.f : PSUM_MAX;
+  const float most = TAKE == CAREFUL && (seen.strict >> lane & 1) ? STRICT : PSUM_MAX;
   const int g = lane / 32;
   f32x16 sc[1];
   scores<T, HD, 1>(kt, q, lane, sc);
@@ -1085,9 +1098,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
     const int whole_to = wave * 32 < rows ? pos_lo + 1 : 0;  // keys before it are seen by every row of the wave
     const int end_key = t.t1 * BKV;
     if (tid == 0) bad = 0;
-    bool careful = false;
+    uint64_t strict = 0;
 #pragma unroll 1
-    for (;;) {
+    for (int pass = 0;; ++pass) {
+      const bool careful = pass > 0;
       st.clear();
       __syncthreads();  // the task (or the pass) before has left LDS
       const lds_mem *mem = (const lds_mem *)&stages[0][0];
@@ -1133,7 +1147,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         const int kt0 = it * BKV;
         if (wave * 32 < rows && kt0 <= pos_hi && kt0 + BKV > first_seen) {
           const Seen seen{pos > far ? pos - far : 0, pos,         last_first, whole_to, t.len, bad != 0, pg,
-                          pages.first,               p.b.ps_div};
+                          pages.first,               p.b.ps_div, strict};
           const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
 #pragma unroll 1
           for (int kb = 32 * taken; kb < BKV; kb += 32)
@@ -1147,9 +1161,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
         ++it;
       }
       // (a barrier after every pass: the next task clears `bad`, which the last tile reads)
-      const bool again = __syncthreads_or(!st.finite());
-      if (careful || !again) break;
-      careful = true;
+      const uint64_t odd = not_finite(st);
+      const bool again = __syncthreads_or(odd != 0);
+      if (pass == 2 || !again) break;
+      if (pass == 1) strict = odd;
     }
 
     const float l = st.l + __shfl_xor(st.l, 32, 64);
@@ -1238,9 +1253,10 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
                                 p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
     if (tid == 0) bad = 0;
-    bool careful = false;
+    uint64_t strict = 0;
 #pragma unroll 1
-    for (;;) {
+    for (int pass = 0;; ++pass) {
+      const bool careful = pass > 0;
       st.clear();
       __syncthreads();  // the task (or the pass) before has left LDS
       // stretches of tiles whose pages fit the staged table
@@ -1252,7 +1268,8 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         const int z = tiles < t.t1 ? (int)tiles : t.t1;
         pages.fill(fp, z * BKV, NT);
         __syncthreads();
-        const Seen seen{pos > far ? pos - far : 0, pos, last_first, pos_lo + 1, t.len, bad != 0, pg, fp, p.b.ps_div};
+        const Seen seen{pos > far ? pos - far : 0, pos, last_first, pos_lo + 1, t.len, bad != 0, pg, fp, p.b.ps_div,
+                        strict};
         const lds_mem *mem = (const lds_mem *)&stages[0][0];
         auto load = [&](int it) {
           const lds_mem *k = mem + ((it - a) & 1) * 2 * TILE;
@@ -1298,8 +1315,9 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
         a = z;
         __syncthreads();
       }
-      if (careful || !__syncthreads_or(!st.finite())) break;
-      careful = true;
+      const uint64_t odd = not_finite(st);
+      if (pass == 2 || !__syncthreads_or(odd != 0)) break;
+      if (pass == 1) strict = odd;
     }
 
     // join the waves: O of wave w at 32 x HD floats w of the stages

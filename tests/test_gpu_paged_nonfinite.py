@@ -1,4 +1,5 @@
-"""crf_paged_attention with values that are no finite numbers."""
+"""crf_paged_attention with values that are no finite numbers: keys that a row does
+not see leave its result as it is to the bit."""
 import math
 
 import pytest
@@ -11,6 +12,56 @@ BF, F32 = "bf16", "f32"
 
 def _dt(name):
     return torch.bfloat16 if name == BF else torch.float32
+
+
+def _run(b, ctx):
+    import paper_2609_30884_amd as crf
+    out = torch.full((b.n_rows, b.nq, b.hd), 7.0, dtype=b.dtype, device="cuda")
+    lse = torch.full((b.n_rows, b.nq), 7.0, dtype=torch.float32, device="cuda")
+    crf.paged_attention(ctx, b.batch, b.q, b.pool, 1, out, lse=lse)
+    torch.cuda.synchronize()
+    assert ctx.device_errors() == 0
+    return out, lse
+
+
+# (new tokens, cached ones): steps and drafts, whose keys the waves share out, and chunks of
+# tiles of 128 rows; prefixes long enough that a row's scores pass 2^4 and 2^16 of its first ones
+SEEN = [
+    (BF, 128, 12, 2, 16, [(3, 1500), (1, 700)], 1), (BF, 64, 8, 2, 7, [(8, 2100)], 4),
+    (F32, 64, 4, 2, 16, [(6, 1200)], 2), (F32, 128, 3, 1, 16, [(9, 1100)], 5),
+    (BF, 128, 12, 2, 16, [(150, 1500), (60, 900)], 90), (BF, 64, 12, 2, 1, [(260, 1100)], 200),
+    (BF, 128, 28, 4, 16, [(400, 3000)], 333), (F32, 64, 4, 2, 16, [(300, 1600)], 140),
+    (F32, 128, 4, 2, 16, [(200, 1800)], 150),
+]
+
+
+@pytest.mark.parametrize("dtype,hd,nq,nkv,page,seqs,first", SEEN)
+@pytest.mark.parametrize("scale", [2.0, 4.0])
+def test_rows_before_a_key_are_as_without_it(dtype, hd, nq, nkv, page, seqs, first, scale):
+    """Token `first` of sequence 0's new ones is no number, in K, V or both: the rows before it keep every bit."""
+    from tests.paged import Batch, context
+    print(f"[case] unseen {dtype} hd {hd} heads {nq}/{nkv} {seqs} queries x {scale}", flush=True)
+    b = Batch(seqs, nq, nkv, hd, _dt(dtype), page=page, seed=41)
+    b.q.mul_(scale)
+    ctx = context(nq, nkv, hd, b.dtype)
+    clean, clean_lse = _run(b, ctx)
+    pg, sl = b.places(0, torch.tensor([seqs[0][1] + first]))
+    keep = torch.ones(b.n_rows, dtype=torch.bool, device="cuda")
+    keep[first:seqs[0][0]] = False
+    pools = [b.k_pool.clone(), b.v_pool.clone()]
+    for odd in (math.nan, math.inf, -math.inf):
+        for which in ("k", "v", "some of v"):
+            if which == "k":
+                b.k_pool[1, pg, :, sl] = odd
+            elif which == "v":
+                b.v_pool[1, pg, :, sl] = odd
+            else:
+                b.v_pool[1, pg, 0, sl, 5::7] = odd
+            got, lse = _run(b, ctx)
+            assert torch.equal(got[keep], clean[keep]), (odd, which)
+            assert torch.equal(lse[keep], clean_lse[keep]), (odd, which)
+            b.k_pool.copy_(pools[0])
+            b.v_pool.copy_(pools[1])
 
 
 @pytest.mark.parametrize("dtype,hd,heads", [(BF, 64, 8), (F32, 64, 4)])
