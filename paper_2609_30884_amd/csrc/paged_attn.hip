@@ -263,7 +263,7 @@ CRF_DEV void scores(const lds_mem *kt, const QFrag<T, HD> &q, int lane, f32x16 (
 // SOME: some row does not see some key, or needs another reference.  CAREFUL: a value
 // that is not finite may belong to a key that some row does not see: the product would
 // multiply it by that row's weight zero, so such values are taken out of the product and
-// added where the weight is not zero.
+// added where the row sees the key (however small its weight: a softmax has no zero).
 //
 // A unit runs without it first, and again with it if some row's result is not finite; the
 // references are raised as before, so that a row that saw none of those values keeps every
@@ -280,9 +280,10 @@ CRF_DEV uint64_t not_finite(const RowState<HD> &st) {
   return m | m >> 32 | m << 32;
 }
 
-// O += P V for the probabilities p of 32 keys (V rows from vt on).
+// O += P V for the probabilities p of 32 keys (V rows from vt on).  CAREFUL: bit v of `on`
+// is set where the row sees the key of p[v].
 template <typename T, int HD, Take TAKE>
-CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, int lane) {
+CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, int lane, uint32_t on_bits = 0) {
   using L = Layout<T, HD>;
   uint32_t va = L::vaddr(lane);
   fresh(va);
@@ -328,7 +329,7 @@ CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, in
             up[e / 4][e % 4] = nan || w == 0x7f80 ? 0x3f80 : 0;
             down[e / 4][e % 4] = nan || w == 0xff80 ? 0x3f80 : 0;
             if (out) x[h][e / 4][e % 4] = 0;
-            on[e] = (float)pf[h][e] != 0.f ? f2bf(1.f) : f2bf(0.f);
+            on[e] = on_bits >> (8 * h + e) & 1 ? f2bf(1.f) : f2bf(0.f);
           }
           plus = mfma32(__builtin_bit_cast(bf16x8, up), on, h == 0 ? zero : plus);
           minus = mfma32(__builtin_bit_cast(bf16x8, down), on, h == 0 ? zero : minus);
@@ -350,7 +351,7 @@ CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, in
         for (int v = 0; v < 16; ++v) plus[v] = minus[v] = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const float on = p[v] != 0.f ? 1.f : 0.f;
+          const float on = on_bits >> v & 1 ? 1.f : 0.f;
           plus = mfma32f(x[v] == INFINITY || x[v] != x[v] ? 1.f : 0.f, on, plus);
           minus = mfma32f(x[v] == -INFINITY || x[v] != x[v] ? 1.f : 0.f, on, minus);
           if (!(fabsf(x[v]) < INFINITY)) x[v] = 0.f;
@@ -487,6 +488,12 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
           if (8 * (v / 4) + 4 * g + v % 4 == i) s[v] = -INFINITY;
     }
   }
+  uint32_t on = 0;
+  if constexpr (TAKE == CAREFUL) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) on |= (s[v] == -INFINITY ? 0u : 1u) << v;
+    fresh(on);  // (one register; else a pair of scalar ones for each bit)
+  }
   float p[16], sum = INFINITY;
   if (!__builtin_amdgcn_ballot_w64(st.ref == -INFINITY)) {
     sum = 0.f;
@@ -516,7 +523,13 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
     if (__builtin_amdgcn_ballot_w64(st.l != 0.f)) {
       st.l *= alpha;
 #pragma unroll
-      for (int b = 0; b < HD / 32; ++b) st.o[b] *= alpha;
+      for (int b = 0; b < HD / 32; ++b) {
+        if constexpr (TAKE == CAREFUL)  // (an infinity stays one, though alpha be zero)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) st.o[b][v] *= fabsf(st.o[b][v]) == INFINITY ? 1.f : alpha;
+        else
+          st.o[b] *= alpha;
+      }
     }
     sum = 0.f;
 #pragma unroll
@@ -526,7 +539,7 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
     }
   }
   st.l += sum;
-  weigh<T, HD, TAKE>(vt, p, st, lane);
+  weigh<T, HD, TAKE>(vt, p, st, lane, on);
 }
 
 // ---------------------------------------------------------------- schedule
@@ -939,6 +952,10 @@ CRF_DEV bool part_done(const PagedAttn &p, const Task &t, int &last) {
   return true;
 }
 
+// What O to the reference `from` weighs next to the reference `to`: never zero, so that its
+// infinities stay (2^-149 of the largest finite number is 2^-21).
+CRF_DEV float rescale(float from, float to) { return fmaxf(fast_exp2(from - to), 0x1p-149f); }
+
 // A row's running result over parts: U parts' references, sums and weights at a time.
 template <int U>
 struct Joined {
@@ -957,16 +974,16 @@ struct Joined {
       some[u] = k0 + u < t.parts && m[u].y != 0.f;
       if (some[u]) top = fmaxf(top, m[u].x);
     }
-    alpha = l == 0.f ? 0.f : fast_exp2(ref - top);
+    alpha = l == 0.f ? 0.f : rescale(ref, top);
     l *= alpha;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      w[u] = some[u] ? fast_exp2(m[u].x - top) : 0.f;
+      w[u] = some[u] ? rescale(m[u].x, top) : 0.f;
       l += w[u] * m[u].y;
     }
     ref = top;
   }
-  CRF_DEV void plus(f32x4 &o, int u, f32x4 x) const {  // (an infinity of no weight stays out)
+  CRF_DEV void plus(f32x4 &o, int u, f32x4 x) const {  // (what is behind the last part stays out)
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = w[u] != 0.f ? fmaf(w[u], x[v], o[v]) : o[v];
   }
@@ -1098,10 +1115,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
     const int whole_to = wave * 32 < rows ? pos_lo + 1 : 0;  // keys before it are seen by every row of the wave
     const int end_key = t.t1 * BKV;
     if (tid == 0) bad = 0;
+    bool careful = false, strictly = false;  // (as a counter: 157 registers spilled instead of 99, fp32 heads of 128)
     uint64_t strict = 0;
 #pragma unroll 1
-    for (int pass = 0;; ++pass) {
-      const bool careful = pass > 0;
+    for (;;) {
       st.clear();
       __syncthreads();  // the task (or the pass) before has left LDS
       const lds_mem *mem = (const lds_mem *)&stages[0][0];
@@ -1163,8 +1180,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
       // (a barrier after every pass: the next task clears `bad`, which the last tile reads)
       const uint64_t odd = not_finite(st);
       const bool again = __syncthreads_or(odd != 0);
-      if (pass == 2 || !again) break;
-      if (pass == 1) strict = odd;
+      if (strictly || !again) break;
+      if (careful) strict = odd;
+      strictly = careful;
+      careful = true;
     }
 
     const float l = st.l + __shfl_xor(st.l, 32, 64);
@@ -1345,7 +1364,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
       for (int w = 0; w < NW; ++w) {
         const float2 m = wml[w][r];
         if (m.y == 0.f) continue;
-        const float k = fast_exp2(m.x - ref);
+        const float k = rescale(m.x, ref);
         l += k * m.y;
         o += k * osum(w)[r * (HD / 4) + (c4 ^ (r & 15))];
       }

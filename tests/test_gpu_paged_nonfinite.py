@@ -1,5 +1,6 @@
 """crf_paged_attention with values that are no finite numbers: keys that a row does
-not see leave its result as it is to the bit."""
+not see leave its result as it is to the bit, and keys that it sees count however
+little they weigh."""
 import math
 
 import pytest
@@ -62,6 +63,38 @@ def test_rows_before_a_key_are_as_without_it(dtype, hd, nq, nkv, page, seqs, fir
             assert torch.equal(lse[keep], clean_lse[keep]), (odd, which)
             b.k_pool.copy_(pools[0])
             b.v_pool.copy_(pools[1])
+
+
+@pytest.mark.parametrize("dtype,hd,nq,seqs", [
+    (BF, 128, 12, [(2, 900), (1, 40)]), (BF, 64, 4, [(4, 2500)]), (F32, 64, 4, [(2, 1500)]), (F32, 128, 4, [(3, 500)]),
+    (BF, 128, 12, [(60, 900), (150, 30)]), (BF, 64, 4, [(100, 2500)]), (F32, 64, 4, [(90, 1500)]),
+    (F32, 128, 4, [(70, 1500)])])
+@pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("order", ["before", "after"])
+def test_values_that_weigh_next_to_nothing(dtype, hd, nq, seqs, odd, order):
+    """A value at a key that is seen counts, also where its weight is e^-400, which no fp32 holds: at the head of a
+    prefix, whose later keys raise the reference, and at its end, in a block of keys that outweigh it."""
+    from tests.paged import Batch, assert_within, attention_reference, context
+    print(f"[case] weightless {dtype} hd {hd} {seqs} {odd} {order}", flush=True)
+    b = Batch(seqs, nq, 2, hd, _dt(dtype), seed=43)
+    b.q.fill_(1.0)
+    b.k_pool.mul_(0.1)
+    low = -400.0 / math.sqrt(hd)  # of every element of a key: a score of -400
+    for s, (n, t) in enumerate(zip(b.new, b.total)):
+        if order == "before":  # blocks of nothing but such keys, of long prefixes whole parts
+            lows, odds = range(t // 2 if t >= 1400 else min(32, t - n)), [0, 20]
+        else:
+            lows = odds = [t - n - 1]
+        pg, sl = b.places(s, torch.tensor(list(lows)))
+        b.k_pool[1, pg, :, sl] = low
+        pg, sl = b.places(s, torch.tensor(odds))
+        b.v_pool[1, pg, :, sl, 3::5] = odd
+    ctx = context(nq, 2, hd, b.dtype)
+    out, lse = _run(b, ctx)
+    ref, rl, bo, bl = attention_reference(b)
+    assert not torch.isfinite(ref).all() and torch.isfinite(ref).any()
+    assert_within(out, ref, bo, "weightless")
+    assert_within(lse, rl, bl, "weightless lse")
 
 
 @pytest.mark.parametrize("dtype,hd,heads", [(BF, 64, 8), (F32, 64, 4)])
