@@ -629,7 +629,7 @@ struct Shape {
     double want;
   };
   __host__ __device__ Plan plan(double total, int units, int longest, int slots) const {
-    const int most = window > 0 && window + bm < longest ? window + bm : longest;
+    const int most = window > 0 && window < longest - bm ? window + bm : longest;
     const float tile = (float)bkv * G, c = ((float)(most + over) * G + bm) / tile, mean = (float)total / tile / slots;
     const int rounds = (units + slots - 1) / slots;
     const float least = sqrtf(c * join);
