@@ -384,7 +384,8 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
  * block tables must already cover, see crf_pages_extend).
  *   q [n_rows][n_q_heads][head_dim], k, v [n_rows][n_kv_heads][head_dim], rows
  *   *_stride elements apart (slices of one fused projection), 16-byte aligned;
- *   q_out may be q; both NULL: keys and values only.
+ *   q_out may be q with q's stride (else it must not overlap the inputs); both
+ *   NULL: keys and values only.
  *   positions: DEVICE int32 [n_rows], rotary positions other than the cache's
  *   (NULL: the cache's).  Angles are reduced in 64 bits at every position.
  * A token on a page out of range raises error bit 0 and is not appended (its q is
@@ -400,7 +401,8 @@ crf_status crf_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq
 /* Softmax attention of every new token over its sequence's pages in layer
  * `layer`: a row at position p sees the keys j <= p, and with window > 0 only
  * those with j > p - window; query head i reads K/V head i / (n_q_heads/n_kv_heads).
- *   q, out [n_rows][n_q_heads][head_dim] as above; out may be q.
+ *   q, out [n_rows][n_q_heads][head_dim] as above; out may be q with q's stride
+ *   (else it must not overlap q).
  *   scale: of the scores (0: 1/sqrt(head_dim)).
  *   lse (nullable): fp32 [n_rows][n_q_heads], the natural logarithm of each row's
  *   sum of exponentials, by which results over parts of a cache can be joined.

@@ -85,6 +85,16 @@ crf_status check_rows(crf_context *ctx, const void *t, int64_t ld, int heads, co
   return CRF_OK;
 }
 
+// In place means the same rows: with another stride a row of the output lies on rows of
+// the queries that other workgroups have yet to read.
+crf_status check_in_place(crf_context *ctx, const crf_seq_batch &b, const void *q, int64_t q_ld, const void *out,
+                          int64_t out_ld, const char *what) {
+  if (q == out && q_ld != out_ld && b.n_rows > 1)
+    return fail(ctx, CRF_ERR_SHAPE, "%s: in place with two strides (%lld, %lld)", what, (long long)q_ld,
+                (long long)out_ld);
+  return CRF_OK;
+}
+
 PagedBatch device_batch(const crf_context *ctx, const crf_seq_batch &b, const crf_page_pool &pool, int layer) {
   PagedBatch d;
   d.row_start = b.row_start;
@@ -226,6 +236,7 @@ crf_status crf_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq
   if (q) {
     if ((st = check_rows(ctx, q, q_stride, d.n_q_heads, "q", what)) != CRF_OK) return st;
     if ((st = check_rows(ctx, q_out, q_out_stride, d.n_q_heads, "q_out", what)) != CRF_OK) return st;
+    if ((st = check_in_place(ctx, *batch, q, q_stride, q_out, q_out_stride, what)) != CRF_OK) return st;
   }
   if ((st = check_rows(ctx, k, k_stride, d.n_kv_heads, "k", what)) != CRF_OK) return st;
   if ((st = check_rows(ctx, v, v_stride, d.n_kv_heads, "v", what)) != CRF_OK) return st;
@@ -268,6 +279,7 @@ crf_status crf_paged_attention(crf_context *ctx, const crf_seq_batch *batch, con
   if (batch->n_seqs == 0 || batch->n_rows == 0) return CRF_OK;
   if ((st = check_rows(ctx, q, q_stride, d.n_q_heads, "q", what)) != CRF_OK) return st;
   if ((st = check_rows(ctx, out, out_stride, d.n_q_heads, "out", what)) != CRF_OK) return st;
+  if ((st = check_in_place(ctx, *batch, q, q_stride, out, out_stride, what)) != CRF_OK) return st;
   if (!aligned4(lse)) return fail(ctx, CRF_ERR_INVALID_ARG, "%s: lse misaligned", what);
   PagedAttn p{};
   p.b = device_batch(ctx, *batch, *pool, layer);

@@ -1,10 +1,13 @@
-"""Host check of how paged attention's launches are planned (no GPU):
-tests/native/paged_plan_check.cpp, compiled against the kernel's source."""
+"""Host checks of paged attention (no GPU), compiled against the sources: how its
+launches are planned (tests/native/paged_plan_check.cpp), and what in place means
+(tests/native/paged_in_place_check.cpp)."""
 import os
 import shutil
 import subprocess
 
 import pytest
+
+from tests.test_schedule_host import _build_and_run
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -23,3 +26,7 @@ def test_plans_of_attention(tmp_path):
     out = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stdout + out.stderr
     assert int(out.stdout.split()[1]) > 8000
+
+
+def test_in_place_means_the_same_rows(tmp_path):
+    assert _build_and_run(tmp_path, "paged_in_place_check") == 12
