@@ -220,8 +220,8 @@ typedef struct {
  * on two internal streams that wait for `stream` and that `stream` then waits
  * for, longest windows first, each on the lane with less work so far; the
  * first such call allocates a second workspace as large as the context's own
- * (what crf_context_create allocates) and two streams, kept until
- * crf_context_destroy.  Otherwise items run in order on `stream`.  Items are
+ * (what crf_context_create allocates, but for the page-pool operators' partials
+ * and counters) and two streams, kept until crf_context_destroy.  Otherwise items run in order on `stream`.  Items are
  * independent when no byte one item may write lies in a range another item
  * may read or write: an item writes the layers [l0, l0+h) of both pools (each
  * layer's whole n_pages*page_stride span, since the pages are chosen by the

@@ -1048,8 +1048,9 @@ void crf_context_destroy(crf_context *ctx) {
   delete ctx;
 }
 
-crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, int32_t max_lora_rank,
-                              crf_context **out) {
+// windows_only: without what the operators over a page pool need.
+static crf_status make_context(const crf_model_dims *dims, int32_t max_tokens, int32_t max_lora_rank,
+                               bool windows_only, crf_context **out) {
   if (!out) return fail(nullptr, CRF_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
   crf_status st = check_dims(nullptr, dims);
@@ -1117,12 +1118,16 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
   } else {
     const size_t ur = max_lora_rank > F32_FUSED_RANK ? 3 * (size_t)max_lora_rank : 0;
     if ((st = dmalloc(ctx, &ctx->u, T * ur * 4)) != CRF_OK) return cleanup(st);
-    ctx->paged_part_floats = PAGED_PART_FLOATS;
-    if ((st = dmalloc(ctx, &ctx->paged_part, (size_t)ctx->paged_part_floats * 4)) != CRF_OK) return cleanup(st);
+    if (!windows_only) {
+      ctx->paged_part_floats = PAGED_PART_FLOATS;
+      if ((st = dmalloc(ctx, &ctx->paged_part, (size_t)ctx->paged_part_floats * 4)) != CRF_OK) return cleanup(st);
+    }
   }
-  if ((st = dmalloc(ctx, &ctx->paged_ws, PAGED_WS_BYTES)) != CRF_OK) return cleanup(st);
-  if (hipMemset(ctx->paged_ws, 0, PAGED_WS_BYTES) != hipSuccess)
-    return cleanup(fail(ctx, CRF_ERR_HIP, "context init: hipMemset"));
+  if (!windows_only) {
+    if ((st = dmalloc(ctx, &ctx->paged_ws, PAGED_WS_BYTES)) != CRF_OK) return cleanup(st);
+    if (hipMemset(ctx->paged_ws, 0, PAGED_WS_BYTES) != hipSuccess)
+      return cleanup(fail(ctx, CRF_ERR_HIP, "context init: hipMemset"));
+  }
   if ((st = dmalloc(ctx, &ctx->rope_cs, T * (dims->head_dim / 2) * sizeof(float2))) != CRF_OK) return cleanup(st);
   if ((st = dmalloc(ctx, &ctx->d_err, sizeof(int))) != CRF_OK) return cleanup(st);
   hipError_t he = hipMemset(ctx->d_err, 0, sizeof(int));
@@ -1131,6 +1136,11 @@ crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, in
   if (he != hipSuccess) return cleanup(fail(ctx, CRF_ERR_HIP, "context init: %s", hipGetErrorString(he)));
   *out = ctx;
   return CRF_OK;
+}
+
+crf_status crf_context_create(const crf_model_dims *dims, int32_t max_tokens, int32_t max_lora_rank,
+                              crf_context **out) {
+  return make_context(dims, max_tokens, max_lora_rank, false, out);
 }
 
 crf_status crf_recompute_window(crf_context *ctx, const crf_model_dims *dims, const void *hidden_at_boundary,
@@ -1206,7 +1216,7 @@ crf_status crf_recompute_window_batched(crf_context *ctx, const crf_model_dims *
   if (!ctx->fork_ev) {  // set last: it marks the lanes complete
     if (!ctx->lane2) {
       crf_context *c2 = nullptr;
-      if (crf_context_create(&ctx->dims, ctx->max_tokens, ctx->max_rank, &c2) != CRF_OK)
+      if (make_context(&ctx->dims, ctx->max_tokens, ctx->max_rank, true, &c2) != CRF_OK)
         return fail(ctx, CRF_ERR_WORKSPACE, "second workspace for concurrent batch items: %s", g_last_error.c_str());
       ctx->lane2 = c2;
     }
