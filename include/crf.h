@@ -332,12 +332,20 @@ typedef struct {
  * Rows past row_start[n_seqs] belong to nobody and are left as they are.
  * row_start [n_seqs+1] (not descending), length [n_seqs] and block_tables
  * [n_seqs][table_stride] are DEVICE int32.  A sequence whose rows or length
- * contradict the bounds below raises error bit 1 and has no new tokens. */
+ * contradict the bounds below raises error bit 1 and has no new tokens.
+ *
+ * max_new and max_pages are all that the host knows of the lengths, and
+ * crf_paged_attention chooses its kernel by them: tiles of 32 rows where
+ * max_new x (n_q_heads/n_kv_heads) is at most 32, or where n_rows and
+ * max_pages x page_size keep the reads of K and V small, else tiles of 128.
+ * Results are right either way, in other last bits; bounds far above what the
+ * batch holds cost time (64 single tokens of 28/4 heads: 154 us with max_new 1,
+ * 196 with 0).  A batch of single tokens should say so. */
 typedef struct {
   int32_t n_seqs;
   int32_t n_rows;       /* rows of the call's tensors                            */
-  int32_t max_new;      /* no sequence has more new tokens (0: n_rows)           */
-  int32_t max_pages;    /* no sequence has more pages                            */
+  int32_t max_new;      /* no sequence has more new tokens (0: n_rows), see above */
+  int32_t max_pages;    /* no sequence has more pages, see above                  */
   int64_t table_stride; /* entries between the rows of block_tables              */
   const int32_t *row_start, *length, *block_tables;
 } crf_seq_batch;
@@ -387,7 +395,8 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
  *   q_out may be q with q's stride (else it must not overlap the inputs); both
  *   NULL: keys and values only.
  *   positions: DEVICE int32 [n_rows], rotary positions other than the cache's
- *   (NULL: the cache's).  Angles are reduced in 64 bits at every position.
+ *   (NULL: the cache's).  Angles are reduced in 64 bits (3e-16 of the angle lost
+ *   at most); cosine, sine and the products are fp32.
  * A token on a page out of range raises error bit 0 and is not appended (its q is
  * still rotated).
  * Errors: INVALID_ARG, SHAPE, RANGE (layer), UNSUPPORTED (rotary_dim above
@@ -408,7 +417,8 @@ crf_status crf_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq
  *   sum of exponentials, by which results over parts of a cache can be joined.
  * Keys on pages out of range are seen by nobody (error bit 0); a row that sees no
  * key gets zeros and lse -inf.  What lies in slots past a sequence's length, or in
- * keys that a row does not see, has no influence on it, numbers or not.  The
+ * keys that a row does not see, has no influence on it, numbers or not; a value
+ * that is no number counts at every key that the row sees, whatever it weighs.  The
  * result is the same to the bit for every call with the same inputs.
  * Errors: INVALID_ARG, SHAPE (negative or non-finite scale, negative window,
  * strides), RANGE (layer), UNSUPPORTED (as crf_rope_append). */
@@ -445,6 +455,8 @@ typedef struct {
  * names a sequence out of range, a child that is not empty or a child that an
  * earlier fork of the call names is skipped (error bit 1), and one for whose page
  * no free page is left (error bit 2); its child stays empty.
+ * A table entry of the parent's that is out of range raises error bit 0: it is
+ * passed on as it is, or (the begun page) not copied.
  * Errors: INVALID_ARG, SHAPE (map and pool differ), UNSUPPORTED. */
 crf_status crf_pages_fork(crf_context *ctx, const crf_page_pool *pool, const crf_page_map *map, int32_t n,
                           const int32_t *parents, const int32_t *children, void *stream);
@@ -459,7 +471,7 @@ crf_status crf_pages_extend(crf_context *ctx, const crf_page_map *map, const int
 /* Ends n sequences (DEVICE int32): their pages are held by one fewer, their
  * length is 0, their table rows are left.  A sequence that is empty or named
  * twice is freed once; one out of range, or a page that nobody holds, raises
- * error bit 1.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED. */
+ * error bit 1, a table entry out of range bit 0.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED. */
 crf_status crf_pages_free(crf_context *ctx, const crf_page_map *map, int32_t n, const int32_t *seqs, void *stream);
 
 /* Moves the pages in use to the front of the pool, in every layer: with L of
@@ -469,6 +481,8 @@ crf_status crf_pages_free(crf_context *ctx, const crf_page_map *map, int32_t n, 
  * the number of pages moved (all DEVICE int32).  The pages moved keep their bytes
  * in their old places, so readers through the old map are right until those are
  * used again.  A table entry that names no page in use becomes -1 (error bit 0).
+ * A sequence whose length passes max_pages or is negative keeps its table row as
+ * it is (error bit 1); map_out's length and row of it are not written.
  * Errors: INVALID_ARG, SHAPE (maps or pool differ), UNSUPPORTED, WORKSPACE. */
 crf_status crf_pages_compact(crf_context *ctx, const crf_page_pool *pool, const crf_page_map *map,
                              const crf_page_map *map_out, int32_t *remap, int32_t *counts, void *stream);

@@ -470,7 +470,8 @@ def _check_pool(d: ModelDims, pool: PagePool, layers: int):
 
 def seq_batch(row_start, length, block_tables, n_rows: int, max_new: int = 0) -> SeqBatch:
     """row_start [S + 1], length [S], block_tables [S, pages]: int32 device tensors; n_rows: rows of the
-    calls' tensors; max_new: the most new tokens of a sequence (0: n_rows)."""
+    calls' tensors; max_new: the most new tokens of a sequence (0: n_rows).  max_new and the tables' width are what
+    paged_attention chooses its kernel by: a batch of single tokens should pass max_new=1."""
     t = _tables(block_tables)
     n = t.shape[0]
     b = SeqBatch(n, int(n_rows), int(max_new), t.shape[1], t.stride(0) if n > 1 else t.shape[1],
