@@ -35,16 +35,16 @@
 // order of the keys (results do not depend on who that is).
 //
 // Measured (bf16, head size 128 where nothing else is said):
-//   8192 tokens after 8192, 28/4 heads    1.38 ms, 1.04 PFLOP/s (a large matrix product
-//     reaches 1.19).  Matrix pipes are busy half of the cycles; with all exponentials of
-//     a tile before its second product, 1.42;
+//   8192 tokens after 8192, 28/4 heads    1.36 ms, 1.06 PFLOP/s (a large matrix product
+//     reaches 1.19).  Matrix pipes are busy 57 % of the cycles; with all exponentials of
+//     a tile before its second product it takes 2.5 % longer;
 //   64 sequences' next tokens over 500 to 16384, 28/4 heads    152 us, 5.2 TB/s: HBM;
 //   12 sequences, some with chunks of up to 512, over up to 8192, 12/2 heads    70 us, 0.43
 //     PFLOP/s: 9 us until the first task is known, 33 of products, 14 to join 9 or 10
 //     parts, whose 33 MB are written and read once;
 //   4 chunks of 500 to 2048 in a window of 1024, 12/2 heads of 64    35 us, 0.43 PFLOP/s:
 //     the exponentials, of which heads of 64 have twice as many to a product;
-//   one next token over 3000, 12/2 heads    13.6 us: a chain of latencies (lengths 2, its
+//   one next token over 3000, 12/2 heads    13.7 us: a chain of latencies (lengths 2, its
 //     schedule 2, page numbers 1.5, keys 3, partials 1.5, ticket 1.5, join 2.5).
 #include <math.h>
 
