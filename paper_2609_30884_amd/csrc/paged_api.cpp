@@ -199,6 +199,7 @@ crf_status crf_rope_init(crf_rope *out, int32_t layout, int32_t rotary_dim, doub
   if (sc.mscale > 0) out->mscale = (float)sc.mscale;
   const double r = rotary_dim;
   if (sc.kind == CRF_ROPE_BASE && rotary_dim > 0) theta *= pow(sc.factor, r / (r - 2));
+  if (!isfinite(theta)) return fail(nullptr, CRF_ERR_SHAPE, "%s: the scaled theta is not finite", what);
   for (int i = 0; i < rotary_dim / 2; ++i) {
     double f = pow(theta, -2.0 * i / r);
     if (sc.kind == CRF_ROPE_LINEAR) f /= sc.factor;
