@@ -519,8 +519,9 @@ def paged_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int
         if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
             raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
     _check_device(ctx, (batch, pool), (q, out, lse))
-    st = ctx.lib.crf_paged_attention(ctx.handle, batch, qp, qs, pool, layer, scale, window, op, os_, _ptr(lse),
-                                     _stream(stream))
+    # (ctypes would take an int's low 32 bits; past the longest sequence a window is none)
+    st = ctx.lib.crf_paged_attention(ctx.handle, batch, qp, qs, pool, layer, scale, min(window, 0x7fffffff), op, os_,
+                                     _ptr(lse), _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 
