@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import Dict, Iterable, List, Mapping, Optional, Sequence, Tuple
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -251,8 +252,16 @@ class Context:
         _err(self.lib, None, self.lib.crf_context_create(ctypes.byref(dims), int(max_tokens), int(max_lora_rank),
                                                           ctypes.byref(h)))
         self.handle = h
-        import torch
-        self.device = torch.cuda.current_device()
+        # (a program that has not imported torch, which brings a HIP runtime of its own, gets along without it)
+        self._device = sys.modules["torch"].cuda.current_device() if "torch" in sys.modules else None
+
+    @property
+    def device(self) -> int:
+        """The device current when the context was made, for checks of the page-pool operators' tensors."""
+        if self._device is None:
+            import torch
+            self._device = torch.cuda.current_device()
+        return self._device
 
     def close(self):
         if getattr(self, "handle", None) and self.handle.value:

@@ -1,4 +1,8 @@
-"""What contexts allocate (the device's free memory before and after)."""
+"""What contexts need: device memory (free before and after), and nothing of torch."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -42,3 +46,15 @@ def test_second_workspace_of_a_batch_holds_no_partials_of_paged_attention():
         assert all(torch.equal(p, q) and torch.equal(p, r) for p, q, r in zip(x, y, z))
     assert ctx.device_errors() == 0
     del first, ctx
+
+
+def test_contexts_of_programs_without_torch():
+    """A program that hands pointers of its own to the library makes contexts without importing torch."""
+    print("[case] no torch", flush=True)
+    code = ("import sys, paper_2609_30884_amd as crf\n"
+            "c = crf.Context(crf.make_dims(2, 128, 2, 2, 64, 64), 16, 0)\n"
+            "assert c.device_errors() == 0 and 'torch' not in sys.modules\n"
+            "c.close()\nprint('made')")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=60,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and r.stdout.strip() == "made", r.stdout + r.stderr
