@@ -426,6 +426,29 @@ crf_status crf_paged_attention(crf_context *ctx, const crf_seq_batch *batch, con
                                const crf_page_pool *pool, int32_t layer, float scale, int32_t window, void *out,
                                int64_t out_stride, float *lse, void *stream);
 
+/* crf_rope_append for models that norm their queries and keys: each head x of q and
+ * k becomes x g / sqrt(mean(x^2) + rms_eps) (RMSNorm over its head_dim elements,
+ * rms_eps of the context's dims) before it is rotated; v is appended as it is.
+ *   q_norm, k_norm: the gains g [head_dim], storage type, 16-byte aligned, one for
+ *   all heads of q and of k (q_norm may be NULL where q is).
+ * Norm, rotation and products are fp32, rounded to the storage type once.
+ * Otherwise as crf_rope_append, its errors included. */
+crf_status crf_norm_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq_batch *batch,
+                                const int32_t *positions, const void *q, int64_t q_stride, const void *k,
+                                int64_t k_stride, const void *v, int64_t v_stride, const void *q_norm,
+                                const void *k_norm, void *q_out, int64_t q_out_stride, const crf_page_pool *pool,
+                                int32_t layer, void *stream);
+
+/* crf_paged_attention for models whose first tokens stay visible: with window > 0 a
+ * row at position p sees the keys j <= p with j > p - window or j < sinks.  Their
+ * pages must still be in the block tables; those between need not be, as long as
+ * their entries name pages of the pool (what lies there is not seen).  window 0:
+ * every key.  Otherwise as crf_paged_attention; with sinks 0 the same to the bit.
+ * Errors: as crf_paged_attention, SHAPE also for negative sinks. */
+crf_status crf_sink_attention(crf_context *ctx, const crf_seq_batch *batch, const void *q, int64_t q_stride,
+                              const crf_page_pool *pool, int32_t layer, float scale, int32_t window, int32_t sinks,
+                              void *out, int64_t out_stride, float *lse, void *stream);
+
 /* Copies pages src[i] of `from` to pages dst[i] of `to` for i < n, in h layers
  * from from_l0 and to_l0 on: a window's layers saved before a refresh overwrites
  * them, or a cache duplicated for another adapter version.  src, dst: DEVICE

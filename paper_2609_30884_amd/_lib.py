@@ -101,7 +101,7 @@ EXPORTS = ("crf_status_string", "crf_abi_version", "crf_context_create", "crf_co
            "crf_context_read_timing",
            "crf_device_info", "crf_decode_logits", "crf_layer_drift_noalloc", "crf_rope_init", "crf_rope_append",
            "crf_paged_attention", "crf_pages_copy", "crf_pages_fork", "crf_pages_extend", "crf_pages_free",
-           "crf_pages_compact")
+           "crf_pages_compact", "crf_norm_rope_append", "crf_sink_attention")
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -155,6 +155,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
             ("rope_init", [P(Rope), I32, I32, ctypes.c_double, P(RopeScaling)]),
             ("rope_append", [VP, P(Rope), P(SeqBatch), VP, VP, I64, VP, I64, VP, I64, VP, I64, P(PagePool), I32, VP]),
             ("paged_attention", [VP, P(SeqBatch), VP, I64, P(PagePool), I32, ctypes.c_float, I32, VP, I64, VP, VP]),
+            ("norm_rope_append", [VP, P(Rope), P(SeqBatch), VP, VP, I64, VP, I64, VP, I64, VP, VP, VP, I64, P(PagePool),
+                                  I32, VP]),
+            ("sink_attention", [VP, P(SeqBatch), VP, I64, P(PagePool), I32, ctypes.c_float, I32, I32, VP, I64, VP,
+                                VP]),
             ("pages_copy", [VP, P(PagePool), I32, P(PagePool), I32, I32, I32, VP, VP, VP]),
             ("pages_fork", [VP, P(PagePool), P(PageMap), I32, VP, VP, VP]),
             ("pages_extend", [VP, P(PageMap), VP, VP]),
@@ -501,9 +505,8 @@ def rope(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "no
     return out
 
 
-def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePool, layer: int, q_out=None,
-                positions=None, stream=None):
-    """crf_rope_append: q rotated into q_out (both None: keys and values only), k rotated and v into the pages."""
+def _append_rows(ctx: Context, batch: SeqBatch, q, k, v, pool: PagePool, layer: int, q_out, positions):
+    """Checks of an append's tensors; positions and the pointer and row stride of q, k, v and q_out."""
     d, n = ctx.dims, batch.n_rows
     _check_pool(ctx.dims, pool, layer + 1)
     qp, qs = _head_rows(d, q, n, d.n_q_heads, "q") if q is not None else (None, 0)
@@ -512,25 +515,69 @@ def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePo
     vp, vs = _head_rows(d, v, n, d.n_kv_heads, "v")
     pp = _int32(positions, n, "positions").data_ptr() if positions is not None else None
     _check_device(ctx, (batch, pool), (q, k, v, q_out, positions))
-    st = ctx.lib.crf_rope_append(ctx.handle, rope, batch, pp, qp, qs, kp, ks, vp, vs, op, os_, pool, layer,
-                                 _stream(stream))
+    return pp, (qp, qs, kp, ks, vp, vs), (op, os_)
+
+
+def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePool, layer: int, q_out=None,
+                positions=None, stream=None):
+    """crf_rope_append: q rotated into q_out (both None: keys and values only), k rotated and v into the pages."""
+    pp, rows, out = _append_rows(ctx, batch, q, k, v, pool, layer, q_out, positions)
+    st = ctx.lib.crf_rope_append(ctx.handle, rope, batch, pp, *rows, *out, pool, layer, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
+
+
+def _gain(d: ModelDims, t, name: str):
+    """Pointer of a head's gains [head_dim] in the storage type."""
+    if t.dtype is not _storage(d):
+        raise CrfError(1, f"{name} is {t.dtype}, the context's storage type differs")
+    if t.shape != (d.head_dim,) or not t.is_contiguous():
+        raise CrfError(2, f"{name} must be a contiguous vector of {d.head_dim}")
+    return t.data_ptr()
+
+
+def norm_rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, q_norm, k_norm, pool: PagePool, layer: int,
+                     q_out=None, positions=None, stream=None):
+    """crf_norm_rope_append: rope_append of q and k whose heads are normed first, with gains q_norm and k_norm
+    [head_dim] (q, q_norm and q_out None: keys and values only)."""
+    pp, rows, out = _append_rows(ctx, batch, q, k, v, pool, layer, q_out, positions)
+    gains = [None if g is None else _gain(ctx.dims, g, name) for g, name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
+    _check_device(ctx, (), (q_norm, k_norm))
+    st = ctx.lib.crf_norm_rope_append(ctx.handle, rope, batch, pp, *rows, *gains, *out, pool, layer, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def _attention_rows(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int, out, lse):
+    """Checks of attention's tensors; pointer and row stride of q and out."""
+    d, n = ctx.dims, batch.n_rows
+    _check_pool(ctx.dims, pool, layer + 1)
+    rows = _head_rows(d, q, n, d.n_q_heads, "q"), _head_rows(d, out, n, d.n_q_heads, "out")
+    if lse is not None:
+        if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
+            raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
+    _check_device(ctx, (batch, pool), (q, out, lse))
+    return rows
+
+
+def _to_int32(n: int) -> int:
+    """ctypes would take an int's low 32 bits; past the longest sequence a number of keys is all of them."""
+    return max(-1, min(n, 0x7fffffff))
 
 
 def paged_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int, out, lse=None, scale: float = 0.0,
                     window: int = 0, stream=None):
     """crf_paged_attention: out [rows, heads, head_dim] (and lse, fp32 [rows, heads]) of the new tokens' queries q."""
-    d, n = ctx.dims, batch.n_rows
-    _check_pool(ctx.dims, pool, layer + 1)
-    qp, qs = _head_rows(d, q, n, d.n_q_heads, "q")
-    op, os_ = _head_rows(d, out, n, d.n_q_heads, "out")
-    if lse is not None:
-        if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
-            raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
-    _check_device(ctx, (batch, pool), (q, out, lse))
-    # (ctypes would take an int's low 32 bits; past the longest sequence a window is none)
-    st = ctx.lib.crf_paged_attention(ctx.handle, batch, qp, qs, pool, layer, scale, min(window, 0x7fffffff), op, os_,
-                                     _ptr(lse), _stream(stream))
+    qr, outr = _attention_rows(ctx, batch, q, pool, layer, out, lse)
+    st = ctx.lib.crf_paged_attention(ctx.handle, batch, *qr, pool, layer, scale, _to_int32(window), *outr, _ptr(lse),
+                                     _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def sink_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int, out, window: int, sinks: int,
+                   lse=None, scale: float = 0.0, stream=None):
+    """crf_sink_attention: paged_attention in a window, besides which every row sees its sequence's first `sinks` keys."""
+    qr, outr = _attention_rows(ctx, batch, q, pool, layer, out, lse)
+    st = ctx.lib.crf_sink_attention(ctx.handle, batch, *qr, pool, layer, scale, _to_int32(window), _to_int32(sinks),
+                                    *outr, _ptr(lse), _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 

@@ -98,6 +98,8 @@ struct RopeAppend {
   int rotary_dim, interleaved;
   float mscale;
   double turns[64];                 // revolutions per position of each pair
+  const void *q_norm, *k_norm;      // gains [hd] of the heads' norms (k_norm null: no norms)
+  float eps;
 };
 hipError_t launch_rope_append(hipStream_t s, bool f32, const RopeAppend &p);
 
@@ -111,6 +113,7 @@ struct PagedAttn {
   int nq, nkv, hd;
   float scale_log2;    // log2(e) * scale
   int window;          // 0: every key
+  int sinks;           // first keys that every later row sees besides its window
   float *part;         // partials of split units
   int64_t part_floats;
   unsigned *tickets;   // PAGED_TICKETS, zero between launches

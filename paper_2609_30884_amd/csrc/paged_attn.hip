@@ -109,6 +109,7 @@ struct Task {
   int seq, kvh, tile;
   int start, n, len;  // first row, new tokens and whole length of the sequence
   int t0, t1;         // key tiles of the part
+  int k0, gap;        // the unit's window begins at tile k0; tiles t before it are the sinks' t - gap
   int parts, part;    // parts of the unit and which this is
   int owner;          // workgroup of the unit's first part
 };
@@ -120,6 +121,7 @@ struct Shape {
   FastDiv g_div;                // by G
   float join;                   // joining a part, in tiles
   bool lead = false;            // `over` lies before a unit's keys, else among them
+  int sinks = 0;                // first keys that are seen besides the window
 
   __host__ __device__ int by_g(int n) const { return (int)(((uint64_t)(uint32_t)n * g_div.mul) >> g_div.shift); }
   __host__ __device__ SeqWork work(int n, int len) const {
@@ -130,7 +132,7 @@ struct Shape {
     w.cap = 0;
     w.below = w.tiles;
     if (window > 0) {
-      w.cap = (double)window * G + bm;
+      w.cap = (double)reach() * G + bm;
       const double room = w.cap - w.base;
       if (room < (double)w.tiles * bm) w.below = room <= 0 ? 0 : (int)((unsigned)room / (unsigned)bm);
     }
@@ -142,6 +144,8 @@ struct Shape {
     const SeqWork w = work(n, len);
     return (units ? (double)w.tiles : w.before(w.tiles)) * nkv;
   }
+  // Keys that a row sees at most.
+  __host__ __device__ int reach() const { return window > INT32_MAX - sinks ? INT32_MAX : window + sinks; }
   __host__ __device__ int first_key(const Task &t) const {  // of the tile's first row
     const int pos = t.len - t.n + by_g(t.tile * bm);
     return window > 0 && pos >= window ? pos - window + 1 : 0;
@@ -161,18 +165,26 @@ struct Shape {
     double want;
   };
   __host__ __device__ Plan plan(double total, int units, int longest, int slots) const {
-    const int most = window > 0 && window < longest - bm ? window + bm : longest;
+    const int most = window > 0 && reach() < longest - bm ? reach() + bm : longest;
     const float tile = (float)bkv * G, c = ((float)(most + over) * G + bm) / tile, mean = (float)total / tile / slots;
     const int rounds = (units + slots - 1) / slots;
     const float least = sqrtf(c * join);
     return Plan{rounds >= MANY || rounds * c <= mean + SPLIT, total / (tile * (least > 1.f ? least : 1.f))};
+  }
+  // The first of a unit's key tiles.  Those of the sinks before its window's first tile k0 count
+  // as if they ended there, so that a part is one run of numbers.
+  __host__ __device__ int first_tile(Task &t) const {
+    t.k0 = first_key(t) / bkv;
+    const int n = sinks / bkv + (sinks % bkv != 0);
+    t.gap = t.k0 - (n < t.k0 ? n : t.k0);
+    return t.gap;
   }
   // Unit i of the sequence's, whole: longest first, its KV heads next to each other.
   __host__ __device__ void whole(int i, Task &t) const {
     const int k = i / nkv;
     t.kvh = i - k * nkv;
     t.tile = work(t.n, t.len).tiles - 1 - k;
-    t.t0 = first_key(t) / bkv;
+    t.t0 = first_tile(t);
     t.t1 = last_key(t) / bkv + 1;
     t.parts = 1;
   }
@@ -196,7 +208,7 @@ struct Shape {
     const double first = w.before(lo), cost = w.before(lo + 1) - first, u0 = seq_base + t.kvh * one + first,
                  u1 = u0 + cost;
     const double stop = u1 < end ? u1 : end;
-    const int k0 = first_key(t) / bkv, k = last_key(t) / bkv + 1 - k0;
+    const int k0 = first_tile(t), k = last_key(t) / bkv + 1 - k0;
     // First key tile of workgroup w's part (both neighbours of a border find it by the same
     // arithmetic).  A first or last part of fewer than SLIVER tiles goes to its neighbour.
     const double ahead = lead ? w.over : 0;
@@ -410,6 +422,8 @@ struct Schedule {
     t.tile = __builtin_amdgcn_readfirstlane(t.tile);
     t.t0 = __builtin_amdgcn_readfirstlane(t.t0);
     t.t1 = __builtin_amdgcn_readfirstlane(t.t1);
+    t.k0 = __builtin_amdgcn_readfirstlane(t.k0);
+    t.gap = __builtin_amdgcn_readfirstlane(t.gap);
     t.parts = __builtin_amdgcn_readfirstlane(t.parts);
     t.owner = __builtin_amdgcn_readfirstlane(t.owner);
     return true;
@@ -519,7 +533,7 @@ struct Joined {
 
 // ---------------------------------------------------------------- tiles of 128 rows
 
-template <typename T, int HD, bool UNI>
+template <typename T, int HD, bool UNI, bool SINKS>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, int slots) {
   using L = Layout<T, HD>;
   constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW, BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * L::ROWB;
@@ -532,7 +546,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
   // A unit costs 256 keys besides its own (with 0 the 12 sequences take 103 us instead of
   // 71, 4096 tokens 156 instead of 91); a part in a join 1.3 tiles, 0.3 of the slower fp32
   // ones (with none 1000 tokens take 38 us instead of 30).
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f, true},
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, sizeof(T) == 2 ? 1.3f : 0.3f, true,
+                     SINKS ? p.sinks : 0},
                slots, true};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
@@ -555,69 +570,78 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(const PagedAttn p, in
                                       p.b.tables + (int64_t)t.seq * p.b.table_stride};
     const int first_seen = pos_lo > far ? pos_lo - far : 0, last_first = pos_hi > far ? pos_hi - far : 0;
     const int whole_to = wave * 32 < rows ? pos_lo + 1 : 0;  // keys before it are seen by every row of the wave
-    const int end_key = t.t1 * BKV;
     if (tid == 0) bad = 0;
     bool careful = false, strictly = false;  // (as a counter: 157 registers spilled instead of 99, fp32 heads of 128)
     uint64_t strict = 0;
 #pragma unroll 1
     for (;;) {
       st.clear();
-      __syncthreads();  // the task (or the pass) before has left LDS
-      const lds_mem *mem = (const lds_mem *)&stages[0][0];
-      auto load = [&](int it, int stage) {
-        const lds_mem *k = mem + stage * 2 * TILE;
-        pages.load(it * BKV + wave * (BKV / NW), k, k + TILE);
-      };
-      if (t.t0 < t.t1) {
-        pages.fill(div_by(t.t0 * BKV, p.b.ps_div), end_key, NT);
+      // the sinks before the window, then the window (else all of the part at once)
+#pragma unroll 1
+      for (int from = t.t0; from < t.t1;) {
+        const bool first = SINKS && from < t.k0;
+        const int to = first ? min(t.t1, t.k0) : t.t1, gap = first ? t.gap : 0;
+        const int ta = from - gap, tz = to - gap, end_key = tz * BKV;
+        from = to;
+        // (keys of the last tile behind the sinks are not loaded)
+        if (SINKS) pages.len = first ? min(t.len, p.sinks) : t.len;
+        __syncthreads();  // the task (or the pass, or the keys) before has left LDS
+        const lds_mem *mem = (const lds_mem *)&stages[0][0];
+        auto load = [&](int it, int stage) {
+          const lds_mem *k = mem + stage * 2 * TILE;
+          pages.load(it * BKV + wave * (BKV / NW), k, k + TILE);
+        };
+        pages.fill(div_by(ta * BKV, p.b.ps_div), end_key, NT);
         __syncthreads();
-        load(t.t0, 0);
-      }
-      // A tile's data is there, the next one's is on its way (each wave passes here once a
-      // tile, wherever it then goes).
-      auto arrive = [&](int it) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (it + 1 < t.t1) {
-          if (div_by(min((it + 2) * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
-            pages.fill(div_by(it * BKV, p.b.ps_div), end_key, NT);
-            __syncthreads();
+        load(ta, 0);
+        // A tile's data is there, the next one's is on its way (each wave passes here once a
+        // tile, wherever it then goes).
+        auto arrive = [&](int it) {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __syncthreads();
+          if (it + 1 < tz) {
+            if (div_by(min((it + 2) * BKV, t.len) - 1, p.b.ps_div) >= pages.first + PGCAP) {
+              pages.fill(div_by(it * BKV, p.b.ps_div), end_key, NT);
+              __syncthreads();
+            }
+            load(it + 1, (it + 1 - ta) & 1);
           }
-          load(it + 1, (it + 1 - t.t0) & 1);
-        }
-      };
-      q.arrived();
+        };
+        q.arrived();
 #pragma unroll 1
-      for (int it = t.t0; it < t.t1;) {
-        // tiles that every row of the wave sees; the first block of all gives the rows
-        // their reference
-        int taken = 0;  // blocks of the tile
-        for (;;) {
-          arrive(it);
+        for (int it = ta; it < tz;) {
+          // tiles that every row of the wave sees; the first block of all gives the rows
+          // their reference
+          int taken = 0;  // blocks of the tile
+          for (;;) {
+            arrive(it);
+            const int kt0 = it * BKV;
+            if (it == ta || kt0 + BKV > whole_to || (kt0 < last_first && !(SINKS && kt0 + BKV <= p.sinks)) || bad ||
+                careful)
+              break;
+            const lds_mem *kt = mem + ((it - ta) & 1) * 2 * TILE;
+            taken = whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane);
+            if (taken < BKV / 32) break;
+            taken = 0;
+            if (++it == tz) break;
+          }
+          if (it == tz) break;
           const int kt0 = it * BKV;
-          if (it == t.t0 || kt0 + BKV > whole_to || kt0 < last_first || bad || careful) break;
-          const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
-          taken = whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, p.scale_log2, lane);
-          if (taken < BKV / 32) break;
-          taken = 0;
-          if (++it == t.t1) break;
-        }
-        if (it == t.t1) break;
-        const int kt0 = it * BKV;
-        if (wave * 32 < rows && kt0 <= pos_hi && kt0 + BKV > first_seen) {
-          const Seen seen{pos > far ? pos - far : 0, pos,         last_first, whole_to, t.len, bad != 0, pg,
-                          pages.first,               p.b.ps_div, strict};
-          const lds_mem *kt = mem + ((it - t.t0) & 1) * 2 * TILE;
+          if (wave * 32 < rows && kt0 <= pos_hi && (kt0 + BKV > first_seen || (SINKS && kt0 < p.sinks))) {
+            const Seen<SINKS> seen{pos > far ? pos - far : 0, pos,         last_first, whole_to, t.len, bad != 0, pg,
+                                   pages.first,               p.b.ps_div, strict,     p.sinks};
+            const lds_mem *kt = mem + ((it - ta) & 1) * 2 * TILE;
 #pragma unroll 1
-          for (int kb = 32 * taken; kb < BKV; kb += 32)
-            if (careful)
-              block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
-                                    seen);
-            else
-              block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
-                                 seen);
+            for (int kb = 32 * taken; kb < BKV; kb += 32)
+              if (careful)
+                block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
+                                      seen);
+              else
+                block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, p.scale_log2, lane,
+                                   seen);
+          }
+          ++it;
         }
-        ++it;
       }
       // (a barrier after every pass: the next task clears `bad`, which the last tile reads)
       const uint64_t odd = not_finite(st);
@@ -681,7 +705,7 @@ struct KeysCfg {
   static constexpr int WG_PER_CU = sizeof(T) * HD * NW * 128 > 65536 ? 1 : 2;
 };
 
-template <typename T, int HD, bool UNI>
+template <typename T, int HD, bool UNI, bool SINKS>
 __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_CU)) void attn_keys_kernel(
     const PagedAttn p, int slots) {
   using L = Layout<T, HD>;
@@ -694,7 +718,8 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 32, l32 = lane % 32;
-  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, 0}, slots, false};
+  Schedule sch{p, Shape{p.nq / p.nkv, p.nkv, p.window, BM, BKV, 256, 0, p.g_div, 0, false, SINKS ? p.sinks : 0}, slots,
+               false};
   const Shape &sh = sch.sh;
   const Partials<HD, BM> parts{p, slots};
   const int far = p.window > 0 ? p.window - 1 : INT32_MAX;
@@ -720,17 +745,22 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
       const bool careful = pass > 0;
       st.clear();
       __syncthreads();  // the task (or the pass) before has left LDS
-      // stretches of tiles whose pages fit the staged table
+      // stretches of tiles whose pages fit the staged table; the sinks before the window are
+      // one of their own
 #pragma unroll 1
-      for (int a = t.t0; a < t.t1;) {
+      for (int from = t.t0; from < t.t1;) {
+        const bool first = SINKS && from < t.k0;
+        const int gap = first ? t.gap : 0, a = from - gap, last_tile = (first ? min(t.t1, t.k0) : t.t1) - gap;
+        // (keys of the last tile behind the sinks are not loaded)
+        if (SINKS) pages.len = first ? min(t.len, p.sinks) : t.len;
         const int fp = div_by(a * BKV, p.b.ps_div);
         // (whole tiles before the end of the staged pages)
         const int64_t tiles = ((int64_t)fp + PGCAP) * p.b.page_size / BKV;
-        const int z = tiles < t.t1 ? (int)tiles : t.t1;
+        const int z = tiles < last_tile ? (int)tiles : last_tile;
         pages.fill(fp, z * BKV, NT);
         __syncthreads();
-        const Seen seen{pos > far ? pos - far : 0, pos, last_first, pos_lo + 1, t.len, bad != 0, pg, fp, p.b.ps_div,
-                        strict};
+        const Seen<SINKS> seen{pos > far ? pos - far : 0, pos, last_first, pos_lo + 1, t.len, bad != 0, pg, fp,
+                               p.b.ps_div,                strict, p.sinks};
         const lds_mem *mem = (const lds_mem *)&stages[0][0];
         auto load = [&](int it) {
           const lds_mem *k = mem + ((it - a) & 1) * 2 * TILE;
@@ -755,7 +785,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
           for (;;) {
             arrive(it);
             const int key0 = it * BKV + wave * 32;
-            if (it == t.t0 || !seen.all(key0) || seen.bad || careful) break;
+            if (it + gap == t.t0 || !seen.all(key0) || seen.bad || careful) break;
             const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
             if (!whole_blocks<T, HD, 1>(kt, kt + TILE, q, st, p.scale_log2, lane)) break;
             leave(it);
@@ -763,7 +793,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
           }
           if (it == z) break;
           const int key0 = it * BKV + wave * 32;
-          if (key0 <= pos_hi && key0 + 32 > first_seen) {
+          if (key0 <= pos_hi && (key0 + 32 > first_seen || (SINKS && key0 < p.sinks))) {
             const lds_mem *kt = mem + ((it - a) & 1) * 2 * TILE + wave * 32 * L::ROWB;
             if (careful)
               block<T, HD, CAREFUL>(kt, kt + TILE, key0, q, st, p.scale_log2, lane, seen);
@@ -773,7 +803,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
           leave(it);
           ++it;
         }
-        a = z;
+        from = z + gap;
         __syncthreads();
       }
       const uint64_t odd = not_finite(st);
@@ -842,7 +872,7 @@ __global__ __launch_bounds__((64 * KeysCfg<T, HD>::NW), (KeysCfg<T, HD>::WG_PER_
   }
 }
 
-template <typename T, int HD, bool UNI>
+template <typename T, int HD, bool UNI, bool SINKS>
 hipError_t launch(hipStream_t s, PagedAttn p) {
   const int G = p.nq / p.nkv;
   // Tiles of 32 rows for up to 32 rows to a sequence and KV head (with tiles of 128 the
@@ -868,15 +898,17 @@ hipError_t launch(hipStream_t s, PagedAttn p) {
   const int64_t grid = !keys && most >= (int64_t)MANY * slots ? most : slots;
   const dim3 g((unsigned)(grid < MOST_GROUPS ? grid : MOST_GROUPS));
   if (keys)
-    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots);
+    hipLaunchKernelGGL((attn_keys_kernel<T, HD, UNI, SINKS>), g, dim3(64 * KeysCfg<T, HD>::NW), 0, s, p, slots);
   else
-    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI>), g, dim3(256), 0, s, p, slots);
+    hipLaunchKernelGGL((attn_rows_kernel<T, HD, UNI, SINKS>), g, dim3(256), 0, s, p, slots);
   return hipGetLastError();
 }
 
 template <typename T, int HD>
 hipError_t launch_uni(hipStream_t s, const PagedAttn &p) {
-  return p.b.page_size % 16 == 0 ? launch<T, HD, true>(s, p) : launch<T, HD, false>(s, p);
+  if (p.window > 0 && p.sinks > 0)
+    return p.b.page_size % 16 == 0 ? launch<T, HD, true, true>(s, p) : launch<T, HD, false, true>(s, p);
+  return p.b.page_size % 16 == 0 ? launch<T, HD, true, false>(s, p) : launch<T, HD, false, false>(s, p);
 }
 
 }  // namespace

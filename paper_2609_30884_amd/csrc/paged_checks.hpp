@@ -167,5 +167,92 @@ crf_status check_copy(crf_context *ctx, const crf_page_pool &p, int layers, cons
   return CRF_OK;
 }
 
+// The checks of an append and what its kernel is given; any: there is something to do.
+crf_status prepare_append(crf_context *ctx, const char *what, const crf_rope *rope, const crf_seq_batch *batch,
+                          const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                          const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, const crf_page_pool *pool,
+                          int32_t layer, RopeAppend &p, bool &any) {
+  crf_status st = check_context(ctx, what);
+  if (st == CRF_OK) st = check_pool(ctx, pool, what);
+  if (st == CRF_OK) st = check_layers(ctx, layer, 1, what);
+  if (st == CRF_OK) st = check_batch(ctx, batch, *pool, what);
+  if (st != CRF_OK) return st;
+  const crf_model_dims &d = ctx->dims;
+  if (!rope) return fail(ctx, CRF_ERR_INVALID_ARG, "%s: rope is NULL", what);
+  if (rope->layout != CRF_ROPE_HALF && rope->layout != CRF_ROPE_INTERLEAVED)
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: unknown layout %d", what, rope->layout);
+  if (rope->rotary_dim < 0 || rope->rotary_dim > d.head_dim || rope->rotary_dim % 16)
+    return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: rotary_dim %d is no multiple of 16 in [0, head_dim]", what,
+                rope->rotary_dim);
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return CRF_OK;
+  if ((q == nullptr) != (q_out == nullptr))
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: q and q_out are given together or not at all", what);
+  if (q) {
+    if ((st = check_rows(ctx, q, q_stride, d.n_q_heads, "q", what)) != CRF_OK) return st;
+    if ((st = check_rows(ctx, q_out, q_out_stride, d.n_q_heads, "q_out", what)) != CRF_OK) return st;
+    if ((st = check_in_place(ctx, *batch, q, q_stride, q_out, q_out_stride, what)) != CRF_OK) return st;
+  }
+  if ((st = check_rows(ctx, k, k_stride, d.n_kv_heads, "k", what)) != CRF_OK) return st;
+  if ((st = check_rows(ctx, v, v_stride, d.n_kv_heads, "v", what)) != CRF_OK) return st;
+  if (!aligned4(positions)) return fail(ctx, CRF_ERR_INVALID_ARG, "%s: positions misaligned", what);
+  p.b = device_batch(ctx, *batch, *pool, layer);
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_out = q_out;
+  p.q_ld = q_stride;
+  p.k_ld = k_stride;
+  p.v_ld = v_stride;
+  p.qo_ld = q_out_stride;
+  p.positions = positions;
+  p.nq = q ? d.n_q_heads : 0;
+  p.nkv = d.n_kv_heads;
+  p.hd = d.head_dim;
+  p.rotary_dim = rope->rotary_dim;
+  p.interleaved = rope->layout == CRF_ROPE_INTERLEAVED;
+  p.mscale = rope->mscale;
+  for (int i = 0; i < rope->rotary_dim / 2; ++i) p.turns[i] = rope->freq[i] / (2 * M_PI);
+  any = true;
+  return CRF_OK;
+}
+
+// The same of attention over the pages.
+crf_status prepare_attention(crf_context *ctx, const char *what, const crf_seq_batch *batch, const void *q,
+                             int64_t q_stride, const crf_page_pool *pool, int32_t layer, float scale, int32_t window,
+                             void *out, int64_t out_stride, float *lse, PagedAttn &p, bool &any) {
+  crf_status st = check_context(ctx, what);
+  if (st == CRF_OK) st = check_pool(ctx, pool, what);
+  if (st == CRF_OK) st = check_layers(ctx, layer, 1, what);
+  if (st == CRF_OK) st = check_batch(ctx, batch, *pool, what);
+  if (st != CRF_OK) return st;
+  const crf_model_dims &d = ctx->dims;
+  if (!(scale >= 0.f) || !isfinite(1.45f * scale))
+    return fail(ctx, CRF_ERR_SHAPE, "%s: scale must be finite and >= 0 (0: 1/sqrt(head_dim))", what);
+  if (window < 0) return fail(ctx, CRF_ERR_SHAPE, "%s: window must be >= 0 (0: every key)", what);
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return CRF_OK;
+  if ((st = check_rows(ctx, q, q_stride, d.n_q_heads, "q", what)) != CRF_OK) return st;
+  if ((st = check_rows(ctx, out, out_stride, d.n_q_heads, "out", what)) != CRF_OK) return st;
+  if ((st = check_in_place(ctx, *batch, q, q_stride, out, out_stride, what)) != CRF_OK) return st;
+  if (!aligned4(lse)) return fail(ctx, CRF_ERR_INVALID_ARG, "%s: lse misaligned", what);
+  p.b = device_batch(ctx, *batch, *pool, layer);
+  p.q = q;
+  p.out = out;
+  p.q_ld = q_stride;
+  p.out_ld = out_stride;
+  p.lse = lse;
+  p.nq = d.n_q_heads;
+  p.nkv = d.n_kv_heads;
+  p.hd = d.head_dim;
+  p.scale_log2 = (float)(1.4426950408889634 * (scale > 0.f ? (double)scale : 1.0 / sqrt((double)d.head_dim)));
+  p.window = window;
+  p.part = ctx->paged_part;
+  p.part_floats = ctx->paged_part_floats;
+  p.tickets = tickets(ctx);
+  p.zeros = zeros(ctx);
+  p.n_cu = ctx->n_cu;
+  any = true;
+  return CRF_OK;
+}
+
 }  // namespace
 }  // namespace crf

@@ -127,7 +127,8 @@ struct QFrag {
 };
 
 // The keys that a lane's row sees: [lo, hi]; bad: some pages of the unit are out of
-// range, whose keys nobody sees.
+// range, whose keys nobody sees.  SINKS: besides them the first `sinks` keys.
+template <bool SINKS>
 struct Seen {
   int lo, hi;
   int all_from, all_to;  // keys that every row of the wave sees: [all_from, all_to)
@@ -137,7 +138,10 @@ struct Seen {
   int first;
   FastDiv ps_div;
   uint64_t strict;  // CAREFUL: lanes whose reference is the maximum
-  CRF_DEV bool all(int key0) const { return key0 >= all_from && key0 + 32 <= all_to; }
+  int sinks;
+  CRF_DEV bool all(int key0) const {
+    return (key0 >= all_from || (SINKS && key0 + 32 <= sinks)) && key0 + 32 <= all_to;
+  }
 };
 
 template <int HD>
@@ -402,9 +406,9 @@ CRF_DEV int whole_blocks(const lds_mem *kt, const lds_mem *vt, const QFrag<T, HD
 }
 
 // One block of 32 keys, key0 ..: scores, probabilities, O += P V.
-template <typename T, int HD, Take TAKE>
+template <typename T, int HD, Take TAKE, bool SINKS>
 CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T, HD> &q, RowState<HD> &st, float c,
-                   int lane, const Seen &seen) {
+                   int lane, const Seen<SINKS> &seen) {
   const float most = TAKE == CAREFUL && (seen.strict >> lane & 1) ? STRICT : PSUM_MAX;
   const int g = lane / 32;
   f32x16 sc[1];
@@ -414,7 +418,7 @@ CRF_DEV void block(const lds_mem *kt, const lds_mem *vt, int key0, const QFrag<T
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int key = key0 + 8 * (v / 4) + 4 * g + v % 4;
-      if (key < seen.lo || key > seen.hi) s[v] = -INFINITY;
+      if ((key < seen.lo && !(SINKS && key < seen.sinks)) || key > seen.hi) s[v] = -INFINITY;
     }
   }
   if (seen.bad) {

@@ -55,7 +55,28 @@ struct Vec<float> {
   }
 };
 
-template <typename T, int TPW>
+// The squares of the N values f of each of a head's n lanes (a power of two, neighbours),
+// to the factor that makes their root mean square one.
+template <int N>
+CRF_DEV float unit_rms(float (&f)[N], int n, float mean, float eps) {
+  auto squares = [&] {
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) ss = fmaf(f[i], f[i], ss);
+    for (int o = n / 2; o >= 1; o /= 2) ss += __shfl_xor(ss, o, 64);
+    return ss;
+  };
+  float ss = squares();
+  if (ss == INFINITY) {  // (values past 2^63: again with smaller ones, next to which eps is nothing)
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] *= 0x1p-80f;
+    ss = squares();
+    eps = 0.f;
+  }
+  return rsqrtf(fmaf(ss, mean, eps));
+}
+
+template <typename T, int TPW, bool NORM>
 __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
   constexpr int E = Vec<T>::E;
   __shared__ int pos_s[TPW], page_s[TPW], slot_s[TPW], seq_s[TPW];
@@ -134,10 +155,23 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
         o1 = o0 + E;
       }
       u32x4 a = ld16(src + o0), c = ld16(src + o1);
-      if (turn) {
+      if (turn || (NORM && !is_v)) {
         float f[2 * E], g[2 * E];
         Vec<T>::unpack(a, f);
         Vec<T>::unpack(c, f + E);
+        if constexpr (NORM) {
+          const T *gain = (const T *)(is_q ? p.q_norm : p.k_norm);
+          Vec<T>::unpack(ld16(gain + o0), g);
+          Vec<T>::unpack(ld16(gain + o1), g + E);
+          const float r = unit_rms(f, uph, 1.f / p.hd, p.eps);
+#pragma unroll
+          for (int e = 0; e < 2 * E; ++e) f[e] = f[e] * r * g[e];
+          if (!turn) {
+            st16(dst + o0, Vec<T>::pack(f));
+            st16(dst + o1, Vec<T>::pack(f + E));
+            continue;
+          }
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float co = cs[j][u * E + e], si = sn[j][u * E + e];
@@ -159,7 +193,7 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
   }
 }
 
-template <typename T>
+template <typename T, bool NORM>
 void launch(hipStream_t s, const RopeAppend &p) {
   const int n = p.b.n_rows;
   // Four tokens a workgroup once workgroups outnumber what the chip holds many times over:
@@ -167,19 +201,20 @@ void launch(hipStream_t s, const RopeAppend &p) {
   // 5.0 / 6.2, 4096 11.0 / 8.6, 16384 32.0 / 22.9; 28 + 2 * 4 heads: 1024 6.3 / 8.8, 2048
   // 9.8 / 10.7, 4096 17.0 / 14.9, 16384 65.9 / 53.1.
   if (n > 2048)
-    hipLaunchKernelGGL((rope_append_kernel<T, 4>), dim3(std::min((n + 3) / 4, MOST_GROUPS)), dim3(NT), 0, s, p);
+    hipLaunchKernelGGL((rope_append_kernel<T, 4, NORM>), dim3(std::min((n + 3) / 4, MOST_GROUPS)), dim3(NT), 0, s, p);
   else
-    hipLaunchKernelGGL((rope_append_kernel<T, 1>), dim3(n), dim3(NT), 0, s, p);
+    hipLaunchKernelGGL((rope_append_kernel<T, 1, NORM>), dim3(n), dim3(NT), 0, s, p);
 }
 
 }  // namespace
 
 hipError_t launch_rope_append(hipStream_t s, bool f32, const RopeAppend &p) {
   if (p.b.n_rows <= 0 || p.b.n_seqs <= 0) return hipSuccess;
+  const bool norm = p.k_norm != nullptr;
   if (f32)
-    launch<float>(s, p);
+    norm ? launch<float, true>(s, p) : launch<float, false>(s, p);
   else
-    launch<bf16>(s, p);
+    norm ? launch<bf16, true>(s, p) : launch<bf16, false>(s, p);
   return hipGetLastError();
 }
 
