@@ -510,9 +510,35 @@ crf_status crf_pages_free(crf_context *ctx, const crf_page_map *map, int32_t n, 
 crf_status crf_pages_compact(crf_context *ctx, const crf_page_pool *pool, const crf_page_map *map,
                              const crf_page_map *map_out, int32_t *remap, int32_t *counts, void *stream);
 
+/* What a row of logits z says of tokens: with lse = ln sum_v e^(z_v) and
+ * ln p_v = z_v - lse, the log probabilities of given tokens, the entropy
+ * -sum_v p_v ln p_v, and the `top` most likely tokens with their log probabilities,
+ * largest first, of equal ones the lowest first.  It takes what crf_decode_logits
+ * returns, or many rows (a prompt scored token by token, a batch's next tokens).
+ *   dtype: of the logits (crf_dtype), whatever the context's;
+ *   logits: [n_rows][vocab], rows row_stride elements apart (any stride >= vocab,
+ *   aligned to their type only);
+ *   tokens, logprob: [n_rows][n_tokens] (dense, n_tokens may be 0).  A token below 0 is
+ *   none and gets 0; one at or past vocab raises error bit 3 and gets -inf;
+ *   entropy, lse: [n_rows], each nullable;
+ *   top_token, top_logprob: [n_rows][top], top at most 32 and at most vocab.
+ * A logit of -inf is a token ruled out: it has probability 0 and adds nothing to the
+ * entropy; a row of nothing else has lse and log probabilities -inf and entropy 0.  A
+ * row that holds NaN or +inf has NaN for lse, entropy and every log probability; among
+ * the most likely NaN comes before +inf.  +0 and -0 are equal.  Sums are fp32.  The
+ * result is the same to the bit for every call with the same inputs.  Takes the
+ * context's workspace, as the operators above (rows that few workgroups would read are
+ * shared out).
+ * Errors: INVALID_ARG, SHAPE (counts, overlapping rows, top above vocab), UNSUPPORTED
+ * (top above 32, vocab above 2^30). */
+crf_status crf_token_logprobs(crf_context *ctx, int32_t dtype, const void *logits, int64_t row_stride, int32_t n_rows,
+                              int32_t vocab, const int32_t *tokens, int32_t n_tokens, float *logprob, float *entropy,
+                              float *lse, int32_t top, int32_t *top_token, float *top_logprob, void *stream);
+
 /* Device-side error flags raised by kernels' own bounds checks since the last
  * call (bit 0: a block table entry outside [0, n_pages); bit 1: a sequence of a
- * batch or page map that contradicts it; bit 2: too few free pages).
+ * batch or page map that contradicts it; bit 2: too few free pages; bit 3: a token
+ * past the vocabulary).
  * Synchronises the device, then clears the flags. */
 crf_status crf_context_device_errors(crf_context *ctx, int32_t *flags_out);
 

@@ -101,7 +101,7 @@ EXPORTS = ("crf_status_string", "crf_abi_version", "crf_context_create", "crf_co
            "crf_context_read_timing",
            "crf_device_info", "crf_decode_logits", "crf_layer_drift_noalloc", "crf_rope_init", "crf_rope_append",
            "crf_paged_attention", "crf_pages_copy", "crf_pages_fork", "crf_pages_extend", "crf_pages_free",
-           "crf_pages_compact", "crf_norm_rope_append", "crf_sink_attention")
+           "crf_pages_compact", "crf_norm_rope_append", "crf_sink_attention", "crf_token_logprobs")
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -159,6 +159,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                   I32, VP]),
             ("sink_attention", [VP, P(SeqBatch), VP, I64, P(PagePool), I32, ctypes.c_float, I32, I32, VP, I64, VP,
                                 VP]),
+            ("token_logprobs", [VP, I32, VP, I64, I32, I32, VP, I32, VP, VP, VP, I32, VP, VP, VP]),
             ("pages_copy", [VP, P(PagePool), I32, P(PagePool), I32, I32, I32, VP, VP, VP]),
             ("pages_fork", [VP, P(PagePool), P(PageMap), I32, VP, VP, VP]),
             ("pages_extend", [VP, P(PageMap), VP, VP]),
@@ -638,4 +639,52 @@ def pages_compact(ctx: Context, pool: PagePool, map: PageMap, map_out: PageMap, 
     rp, cp = _int32(remap, map.n_pages, "remap").data_ptr(), _int32(counts, 2, "counts").data_ptr()
     _check_device(ctx, (pool, map, map_out), (remap, counts))
     st = ctx.lib.crf_pages_compact(ctx.handle, pool, map, map_out, rp, cp, _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+# ----------------------------------------------------------------------------- what logits say of tokens
+
+def _values(t, shape, dtype, name: str):
+    """Pointer of a contiguous tensor of that type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise CrfError(2, f"{name} must be contiguous {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def token_logprobs(ctx: Context, logits, tokens=None, logprob=None, entropy=None, lse=None, top_token=None,
+                   top_logprob=None, stream=None):
+    """crf_token_logprobs of logits [rows, vocab] (fp32 or bf16, contiguous rows; [vocab]: one row), into what is given:
+    logprob (fp32) of tokens (int32) [rows, n] or [rows], entropy and lse (fp32) [rows], and the most likely tokens
+    top_token (int32) with top_logprob (fp32) [rows, top]."""
+    import torch
+    if logits.dim() == 1:
+        logits = logits[None]
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise CrfError(2, f"logits must be float32 or bfloat16 [rows, vocab] with contiguous rows, not {logits.dtype} "
+                          f"{tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    if (tokens is None) != (logprob is None) or (top_token is None) != (top_logprob is None):
+        raise CrfError(1, "tokens and logprob, top_token and top_logprob are given together or not at all")
+    n = top = 0
+    if tokens is not None:
+        if tokens.dim() not in (1, 2) or tokens.shape[0] != rows:
+            raise CrfError(2, f"tokens {tuple(tokens.shape)} are not those of {rows} rows")
+        n = 1 if tokens.dim() == 1 else tokens.shape[1]
+    if top_token is not None:
+        if top_token.dim() != 2:
+            raise CrfError(2, "top_token must be [rows, top]")
+        top = top_token.shape[1]
+    f32, i32 = torch.float32, torch.int32
+    tp = _values(tokens, tokens.shape if n else None, i32, "tokens") if n else None
+    lp = _values(logprob, tokens.shape, f32, "logprob") if n else None
+    ep, sp = _values(entropy, (rows,), f32, "entropy"), _values(lse, (rows,), f32, "lse")
+    kp = _values(top_token, (rows, top), i32, "top_token") if top else None
+    vp = _values(top_logprob, (rows, top), f32, "top_logprob") if top else None
+    _check_device(ctx, (), (logits, tokens, logprob, entropy, lse, top_token, top_logprob))
+    st = ctx.lib.crf_token_logprobs(ctx.handle, CRF_F32 if logits.dtype is f32 else CRF_BF16, logits.data_ptr(),
+                                    logits.stride(0) if rows > 1 else vocab, rows, vocab, tp, n, lp, ep, sp, top, kp, vp,
+                                    _stream(stream))
     _err(ctx.lib, ctx.handle, st)

@@ -6,6 +6,7 @@
 #include "context.hpp"
 #include "paged.hpp"
 #include "paged_checks.hpp"
+#include "serving.hpp"
 
 using namespace crf;
 
@@ -46,6 +47,52 @@ crf_status crf_sink_attention(crf_context *ctx, const crf_seq_batch *batch, cons
   p.sinks = sinks;
   LAUNCH(ctx, (hipStream_t)stream, CRF_KK_ATTN,
          launch_paged_attn((hipStream_t)stream, ctx->dims.dtype == CRF_F32, p));
+  return CRF_OK;
+}
+
+crf_status crf_token_logprobs(crf_context *ctx, int32_t dtype, const void *logits, int64_t row_stride, int32_t n_rows,
+                              int32_t vocab, const int32_t *tokens, int32_t n_tokens, float *logprob, float *entropy,
+                              float *lse, int32_t top, int32_t *top_token, float *top_logprob, void *stream) {
+  const char *what = "crf_token_logprobs";
+  crf_status st = check_context(ctx, what);
+  if (st != CRF_OK) return st;
+  if (dtype != CRF_F32 && dtype != CRF_BF16)
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: unknown dtype %d", what, dtype);
+  if (n_rows < 0 || vocab < 1 || n_tokens < 0 || top < 0 || top > vocab)
+    return fail(ctx, CRF_ERR_SHAPE, "%s: n_rows, n_tokens and top >= 0, vocab >= 1 and top <= vocab", what);
+  if (top > LOGP_MAX_TOP) return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: top %d above %d", what, top, LOGP_MAX_TOP);
+  if (vocab > 1 << 30) return fail(ctx, CRF_ERR_UNSUPPORTED, "%s: more than 2^30 logits a row", what);
+  if (row_stride < vocab && n_rows > 1)
+    return fail(ctx, CRF_ERR_SHAPE, "%s: the rows of logits overlap (stride %lld)", what, (long long)row_stride);
+  if (n_rows == 0) return CRF_OK;
+  const uintptr_t esz = dtype == CRF_F32 ? 4 : 2;
+  if (!logits || (uintptr_t)logits % esz)
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: logits NULL or misaligned", what);
+  if (n_tokens > 0 && (!tokens || !logprob || !aligned4(tokens) || !aligned4(logprob)))
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: tokens or logprob NULL or misaligned", what);
+  if (top > 0 && (!top_token || !top_logprob || !aligned4(top_token) || !aligned4(top_logprob)))
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: top_token or top_logprob NULL or misaligned", what);
+  if (!aligned4(entropy) || !aligned4(lse))
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: entropy or lse misaligned", what);
+  TokenLogprobs p{};
+  p.logits = logits;
+  p.ld = row_stride;
+  p.n_rows = n_rows;
+  p.vocab = vocab;
+  p.tokens = tokens;
+  p.n_tokens = n_tokens;
+  p.top = top;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.lse = lse;
+  p.top_token = top_token;
+  p.top_logprob = top_logprob;
+  p.part = ctx->paged_part;
+  p.part_floats = ctx->paged_part ? ctx->paged_part_floats : 0;
+  p.tickets = tickets(ctx);
+  p.n_tickets = PAGED_TICKETS;
+  p.err = ctx->d_err;
+  LAUNCH(ctx, (hipStream_t)stream, CRF_KK_OTHER, launch_token_logprobs((hipStream_t)stream, dtype == CRF_F32, p));
   return CRF_OK;
 }
 
