@@ -449,6 +449,32 @@ crf_status crf_sink_attention(crf_context *ctx, const crf_seq_batch *batch, cons
                               const crf_page_pool *pool, int32_t layer, float scale, int32_t window, int32_t sinks,
                               void *out, int64_t out_stride, float *lse, void *stream);
 
+/* Sequences of a batch that share their first tokens, as crf_pages_fork leaves them.
+ * Group g is the sequences seq_start[g] .. seq_start[g+1]-1 of the batch, whose first
+ * shared_len[g] tokens have the same keys and values (on the same pages, or on copies
+ * of them), which are read through the first one's block table; that sequence need not
+ * have new tokens.  DEVICE int32: seq_start [n_groups+1] (ascending), shared_len
+ * [n_groups].  Sequences before seq_start[0] and from seq_start[n_groups] on are in no
+ * group.  A group that contradicts the batch (its sequences or rows descend or are out
+ * of range, its first sequence is shorter than shared_len) raises error bit 1 and
+ * shares nothing. */
+typedef struct {
+  int32_t n_groups;
+  const int32_t *seq_start, *shared_len;
+} crf_seq_groups;
+
+/* crf_paged_attention (without a window) of a batch in groups, whose shared keys and
+ * values are read once for all of a group's new tokens.  The same attention, in other
+ * last bits; the same to the bit for every call with the same inputs.  It pays where
+ * sequences bring few tokens each; a batch whose sequences may bring more than 128 /
+ * (n_q_heads/n_kv_heads) (max_new), with more than 1023 groups, or whose parts the context's workspace
+ * does not hold, is computed by crf_paged_attention's kernels, which do not look at the
+ * groups.
+ * Errors: as crf_paged_attention, SHAPE also for more groups than sequences. */
+crf_status crf_shared_attention(crf_context *ctx, const crf_seq_batch *batch, const crf_seq_groups *groups,
+                                const void *q, int64_t q_stride, const crf_page_pool *pool, int32_t layer, float scale,
+                                void *out, int64_t out_stride, float *lse, void *stream);
+
 /* Copies pages src[i] of `from` to pages dst[i] of `to` for i < n, in h layers
  * from from_l0 and to_l0 on: a window's layers saved before a refresh overwrites
  * them, or a cache duplicated for another adapter version.  src, dst: DEVICE

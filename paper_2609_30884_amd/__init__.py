@@ -10,5 +10,5 @@ from ._lib import (  # noqa: F401
     device_info, decode_logits,
     PageMap, PagePool, Rope, SeqBatch, page_map, page_pool, paged_attention, pages_compact, pages_copy, pages_extend,
     pages_fork, pages_free, rope, rope_append, seq_batch,
-    norm_rope_append, sink_attention, token_logprobs,
+    SeqGroups, norm_rope_append, seq_groups, shared_attention, sink_attention, token_logprobs,
 )

@@ -75,6 +75,10 @@ class SeqBatch(ctypes.Structure):
                 ("row_start", ctypes.c_void_p), ("length", ctypes.c_void_p), ("block_tables", ctypes.c_void_p)]
 
 
+class SeqGroups(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("seq_start", ctypes.c_void_p), ("shared_len", ctypes.c_void_p)]
+
+
 class Rope(ctypes.Structure):
     _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("mscale", ctypes.c_float),
                 ("freq", ctypes.c_double * 64)]
@@ -101,7 +105,8 @@ EXPORTS = ("crf_status_string", "crf_abi_version", "crf_context_create", "crf_co
            "crf_context_read_timing",
            "crf_device_info", "crf_decode_logits", "crf_layer_drift_noalloc", "crf_rope_init", "crf_rope_append",
            "crf_paged_attention", "crf_pages_copy", "crf_pages_fork", "crf_pages_extend", "crf_pages_free",
-           "crf_pages_compact", "crf_norm_rope_append", "crf_sink_attention", "crf_token_logprobs")
+           "crf_pages_compact", "crf_norm_rope_append", "crf_sink_attention", "crf_shared_attention",
+           "crf_token_logprobs")
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -159,6 +164,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                   I32, VP]),
             ("sink_attention", [VP, P(SeqBatch), VP, I64, P(PagePool), I32, ctypes.c_float, I32, I32, VP, I64, VP,
                                 VP]),
+            ("shared_attention", [VP, P(SeqBatch), P(SeqGroups), VP, I64, P(PagePool), I32, ctypes.c_float, VP, I64, VP,
+                                  VP]),
             ("token_logprobs", [VP, I32, VP, I64, I32, I32, VP, I32, VP, VP, VP, I32, VP, VP, VP]),
             ("pages_copy", [VP, P(PagePool), I32, P(PagePool), I32, I32, I32, VP, VP, VP]),
             ("pages_fork", [VP, P(PagePool), P(PageMap), I32, VP, VP, VP]),
@@ -579,6 +586,25 @@ def sink_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int,
     qr, outr = _attention_rows(ctx, batch, q, pool, layer, out, lse)
     st = ctx.lib.crf_sink_attention(ctx.handle, batch, *qr, pool, layer, scale, _to_int32(window), _to_int32(sinks),
                                     *outr, _ptr(lse), _stream(stream))
+    _err(ctx.lib, ctx.handle, st)
+
+
+def seq_groups(seq_start, shared_len) -> SeqGroups:
+    """seq_start [G + 1], shared_len [G]: int32 device tensors; sequences seq_start[g] .. seq_start[g + 1] - 1 of a batch
+    share the keys and values of their first shared_len[g] tokens."""
+    n = shared_len.numel()
+    g = SeqGroups(n, _int32(seq_start, n + 1, "seq_start").data_ptr(), _int32(shared_len, n, "shared_len").data_ptr())
+    g.tensors, g.device = (seq_start, shared_len), _same_device(seq_start, shared_len)
+    return g
+
+
+def shared_attention(ctx: Context, batch: SeqBatch, groups: SeqGroups, q, pool: PagePool, layer: int, out, lse=None,
+                     scale: float = 0.0, stream=None):
+    """crf_shared_attention: paged_attention of a batch in groups whose shared keys are read once."""
+    qr, outr = _attention_rows(ctx, batch, q, pool, layer, out, lse)
+    _check_device(ctx, (groups,), ())
+    st = ctx.lib.crf_shared_attention(ctx.handle, batch, groups, *qr, pool, layer, scale, *outr, _ptr(lse),
+                                      _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 

@@ -33,4 +33,19 @@ struct TokenLogprobs {
 };
 hipError_t launch_token_logprobs(hipStream_t s, bool f32, const TokenLogprobs &p);
 
+// ---------------------------------------------------------------- attention over shared prefixes
+constexpr int SHARED_MAX_GROUPS = 1023;
+
+struct SharedAttn {
+  PagedAttn a;  // the batch (no window)
+  int n_groups;
+  const int32_t *seq_start, *shared_len;  // [n_groups + 1], [n_groups]
+  // set by the launcher: the items' table, and the parts' O [part_rows][hd] and (reference, sum)
+  void *info;
+  float *o;
+  float2 *ml;
+  int part_rows, slots;
+};
+hipError_t launch_shared_attn(hipStream_t s, bool f32, SharedAttn p);
+
 }  // namespace crf

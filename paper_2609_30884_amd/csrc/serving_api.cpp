@@ -50,6 +50,31 @@ crf_status crf_sink_attention(crf_context *ctx, const crf_seq_batch *batch, cons
   return CRF_OK;
 }
 
+crf_status crf_shared_attention(crf_context *ctx, const crf_seq_batch *batch, const crf_seq_groups *groups,
+                                const void *q, int64_t q_stride, const crf_page_pool *pool, int32_t layer, float scale,
+                                void *out, int64_t out_stride, float *lse, void *stream) {
+  const char *what = "crf_shared_attention";
+  SharedAttn p{};
+  bool any = false;
+  crf_status st = prepare_attention(ctx, what, batch, q, q_stride, pool, layer, scale, 0, out, out_stride, lse, p.a,
+                                    any);
+  if (st != CRF_OK) return st;
+  if (!groups) return fail(ctx, CRF_ERR_INVALID_ARG, "%s: the groups are NULL", what);
+  if (groups->n_groups < 0) return fail(ctx, CRF_ERR_SHAPE, "%s: n_groups must be >= 0", what);
+  if (groups->n_groups > batch->n_seqs)
+    return fail(ctx, CRF_ERR_SHAPE, "%s: %d groups of %d sequences", what, groups->n_groups, batch->n_seqs);
+  if (!any) return CRF_OK;
+  if (groups->n_groups > 0 && (!groups->seq_start || !groups->shared_len || !aligned4(groups->seq_start) ||
+                               !aligned4(groups->shared_len)))
+    return fail(ctx, CRF_ERR_INVALID_ARG, "%s: seq_start or shared_len NULL or misaligned", what);
+  p.n_groups = groups->n_groups;
+  p.seq_start = groups->seq_start;
+  p.shared_len = groups->shared_len;
+  LAUNCH(ctx, (hipStream_t)stream, CRF_KK_ATTN,
+         launch_shared_attn((hipStream_t)stream, ctx->dims.dtype == CRF_F32, p));
+  return CRF_OK;
+}
+
 crf_status crf_token_logprobs(crf_context *ctx, int32_t dtype, const void *logits, int64_t row_stride, int32_t n_rows,
                               int32_t vocab, const int32_t *tokens, int32_t n_tokens, float *logprob, float *entropy,
                               float *lse, int32_t top, int32_t *top_token, float *top_logprob, void *stream) {
