@@ -28,13 +28,15 @@ namespace {
 
 constexpr int NT = 256, NW = NT / 64;
 constexpr int BATCH = 4;                    // 16-byte loads of a thread in flight
-constexpr int LIST = 64 * 8 + LOGP_MAX_TOP; // keys of a wave: a step's, and k
+constexpr int LIST = 128;                   // keys of a wave: k, and one to a lane
+static_assert(LOGP_MAX_TOP + 64 <= LIST, "keys");
 constexpr float LOG2E = 1.4426950408889634f;
 // Workgroups that a row is shared out to: until there are FILL of them, none smaller than
 // SMALLEST loads of 16 bytes.
-constexpr int FILL = 1024, SMALLEST = 256;
+constexpr int FILL = 512, SMALLEST = 512;
 
 typedef unsigned long long Key;  // order of the value, ~index; 0: none
+typedef __attribute__((address_space(3))) Key lds_key;
 
 // Values in their order as integers: NaN above all, -0 as +0; none is 0.
 CRF_DEV uint32_t order(float z) {
@@ -43,10 +45,6 @@ CRF_DEV uint32_t order(float z) {
 }
 CRF_DEV float value(uint32_t o) { return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 CRF_DEV Key key(float z, int index) { return (Key)order(z) << 32 | (uint32_t)~index; }
-CRF_DEV Key lane_key(Key v, int lane) {
-  return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
-}
 CRF_DEV int bits_below(uint64_t m) {  // bits of m below this lane
   return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
 }
@@ -58,50 +56,71 @@ CRF_DEV void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Puts the k largest of the wave's n <= LIST keys in front, largest first; returns how many.
-CRF_DEV int keep_largest(Key *list, int n, int k, int lane) {
-  constexpr int PER = (LIST + 63) / 64;
-  wave_order();
-  Key own[PER], most = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    own[i] = i * 64 + lane < n ? list[i * 64 + lane] : 0;
-    most = own[i] > most ? own[i] : most;
-  }
-  if (n > 64) {
-    // no key below the k-th largest of the lanes' largest is one of the k
-    int above = 0;
+// The largest number of the leading BITS bits that at least k of the lanes' values reach.
+template <int BITS>
+CRF_DEV uint32_t reached_by(uint32_t v, int k) {
+  uint32_t least = 0;
 #pragma unroll 4
-    for (int l = 0; l < 64; ++l) above += lane_key(most, l) > most;
-    const Key least = lane_key(most, __builtin_ctzll(__builtin_amdgcn_ballot_w64(above == k - 1)));
-    n = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool stays = own[i] >= least;
-      const uint64_t m = __builtin_amdgcn_ballot_w64(stays);
-      if (stays) list[n + bits_below(m)] = own[i];
-      n += __popcll(m);
-    }
-    wave_order();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) own[i] = i * 64 + lane < n ? list[i * 64 + lane] : 0;
+  for (int b = 31; b > 31 - BITS; --b) {
+    const uint32_t more = least | 1u << b;
+    if (__popcll(__builtin_amdgcn_ballot_w64(v >= more)) >= k) least = more;
   }
-  int rank[PER];
+  return least;
+}
+
+// How many of the n <= 64 keys that the wave's lanes hold are larger than the lane's own;
+// `keys` is room for 64.
+CRF_DEV int place(Key own, lds_key *keys, int n) {
+  const int lane = threadIdx.x % 64;
+  keys[lane] = lane < n ? own : 0;
+  wave_order();
+  int rank = 0;
+#pragma unroll 1
+  for (int l = 0; l < n; l += 8) {
+    Key other[8];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) rank[i] = 0;
-  if (n <= 64) {
-    for (int l = 0; l < n; ++l) rank[0] += lane_key(own[0], l) > own[0];
-  } else {
-    for (int l = 0; l < n; ++l) {
-      const Key other = list[l];
+    for (int i = 0; i < 8; ++i) other[i] = keys[l + i];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) rank[i] += other > own[i];
-    }
+    for (int i = 0; i < 8; ++i) rank += other[i] > own;
   }
   wave_order();
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (own[i] && rank[i] < k) list[rank[i]] = own[i];
+  return rank;
+}
+
+// Puts the k largest of the wave's n <= LIST keys in front, largest first; returns how many.
+CRF_DEV int keep_largest(lds_key *list, int n, int k) {
+  const int lane = threadIdx.x % 64;
+  wave_order();
+  Key a = lane < n ? list[lane] : 0, b = lane + 64 < n ? list[lane + 64] : 0;
+  wave_order();
+  if (n > 64) {
+    // a value that k of the lanes' larger ones reach: no key below it is one of the k
+    const Key least = (Key)reached_by<32>((uint32_t)((a > b ? a : b) >> 32), k) << 32;
+    const uint64_t ma = __builtin_amdgcn_ballot_w64(a >= least && a), mb = __builtin_amdgcn_ballot_w64(b >= least && b);
+    const int na = __popcll(ma), both = na + __popcll(mb);
+    if (both <= 64) {
+      if (ma >> lane & 1) list[bits_below(ma)] = a;
+      if (mb >> lane & 1) list[na + bits_below(mb)] = b;
+      wave_order();
+      n = both;
+      a = lane < n ? list[lane] : 0;
+      wave_order();
+    } else {  // (equal values: each key's place among all of them)
+      int ra = 0, rb = 0;
+      for (int l = 0; l < n; ++l) {
+        const Key other = list[l];
+        ra += other > a;
+        rb += other > b;
+      }
+      wave_order();
+      if (a && ra < k) list[ra] = a;
+      if (b && rb < k) list[rb] = b;
+      wave_order();
+      return k;
+    }
+  }
+  const int rank = place(a, list, n);
+  if (a && rank < k) list[rank] = a;
   wave_order();
   return n < k ? n : k;
 }
@@ -122,17 +141,30 @@ struct Sums {
   }
   // Over the wave's lanes, in one order.
   CRF_DEV void wave() {
-    to(wave_max(m));
-    s = wave_sum(s);
-    w = wave_sum(w);
+    float most = m;
+    wave_prefix([&](auto c, auto rows) {
+      const int v = __builtin_bit_cast(int, most);
+      most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, c(), rows(), 0xf, false)));
+    });
+    to(last(most));
+    wave_prefix([&](auto c, auto rows) {
+      s += __builtin_bit_cast(float, from_lane<c(), rows()>(__builtin_bit_cast(int, s)));
+      w += __builtin_bit_cast(float, from_lane<c(), rows()>(__builtin_bit_cast(int, w)));
+    });
+    s = last(s);
+    w = last(w);
+  }
+  static CRF_DEV float last(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
   }
 };
 
 template <typename T>
-struct Elements;  // 16 bytes as floats
+struct Elements;  // 16 bytes as floats; NONE: -inf in all of them
 template <>
 struct Elements<float> {
   static constexpr int N = 4;
+  static constexpr uint32_t NONE = 0xff800000u;
   static CRF_DEV void get(u32x4 v, float *f) {
     const f32x4 x = __builtin_bit_cast(f32x4, v);
 #pragma unroll
@@ -142,6 +174,7 @@ struct Elements<float> {
 template <>
 struct Elements<bf16> {
   static constexpr int N = 8;
+  static constexpr uint32_t NONE = 0xff80ff80u;
   static CRF_DEV void get(u32x4 v, float *f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -178,123 +211,184 @@ struct Part {
 };
 
 template <typename T, bool TOP>
-__global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs p, int parts) {
+__global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogprobs p, int parts, int each) {
   constexpr int E = Elements<T>::N;
   __shared__ Sums wave_sums[NW];
   __shared__ Key lists[TOP ? NW : 1][TOP ? LIST : 1];
-  __shared__ Key best[TOP ? LOGP_MAX_TOP : 1];
+  __shared__ Key best[TOP ? LOGP_MAX_TOP : 1], flat[TOP ? 64 : 1];
+  // a batch's loads that hold something to enter, with their numbers; then the parts' keys
+  __shared__ __align__(16) u32x4 held[TOP ? NW : 1][TOP ? BATCH * 64 : 1];
+  __shared__ uint16_t held_at[TOP ? NW : 1][TOP ? BATCH * 64 : 1];
+  __shared__ uint32_t reach[NW];
+  __shared__ int count[NW];
   __shared__ int last;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int k = p.top, V = p.vocab;
-  Key *const list = lists[TOP ? wave : 0];
+  lds_key *const list = (lds_key *)lists[TOP ? wave : 0];
+  const float per_k = 1.f / (TOP ? k : 1);
 
-  // The k largest of the waves' lists, each sorted, of n[w] <= k keys.
+  // The k largest of the waves' lists of n keys each into `best`, largest first.
   auto join_waves = [&](int n) {
-    if (lane < LOGP_MAX_TOP && lane >= n) list[lane] = 0;
+    if (lane == 0) count[wave] = n;
     if (tid < LOGP_MAX_TOP) best[tid] = 0;
     __syncthreads();
-    if (tid < NW * LOGP_MAX_TOP) {
-      const Key own = lists[TOP ? tid / LOGP_MAX_TOP : 0][TOP ? tid % LOGP_MAX_TOP : 0];
-      int rank = 0;
+    int start[NW], all = 0;
 #pragma unroll
-      for (int w = 0; w < NW; ++w)
-#pragma unroll 8
-        for (int i = 0; i < LOGP_MAX_TOP; ++i) rank += lists[TOP ? w : 0][TOP ? i : 0] > own;
-      if (own && rank < k) best[rank] = own;
+    for (int w = 0; w < NW; ++w) {
+      start[w] = all;
+      all += count[w];
+    }
+    if (__builtin_amdgcn_readfirstlane(all) <= 64) {  // a lane to each
+      if (wave == 0) {
+        int w = 0;
+#pragma unroll
+        for (int i = 1; i < NW; ++i) w = lane >= start[i] ? i : w;
+        int first = start[0];
+#pragma unroll
+        for (int i = 1; i < NW; ++i) first = w == i ? start[i] : first;
+        const Key own = lane < all ? lists[w][lane - first] : 0;
+        const int rank = place(own, (lds_key *)flat, all);
+        if (own && rank < k) best[rank] = own;
+      }
+    } else {
+      n = keep_largest(list, n, k);
+      if (lane < LOGP_MAX_TOP && lane >= n) list[lane] = 0;
+      __syncthreads();
+      if (tid < NW * LOGP_MAX_TOP) {
+        // a key's place is its own in its list and how many are larger in the others
+        const int w = tid / LOGP_MAX_TOP, i = tid % LOGP_MAX_TOP;
+        const Key own = lists[w][i];
+        int rank = i;
+#pragma unroll
+        for (int o = 1; o < NW; ++o) {
+          const Key *other = lists[(w + o) % NW];
+          int larger = 0;
+#pragma unroll
+          for (int size = LOGP_MAX_TOP / 2; size >= 1; size /= 2)
+            if (other[larger + size - 1] > own) larger += size;
+          rank += larger + (other[larger] > own);
+        }
+        if (own && rank < k) best[rank] = own;
+      }
     }
     __syncthreads();
   };
+  // The least of the waves' numbers.
+  auto least_of_waves = [&](uint32_t v) {
+    if (lane == 0) reach[wave] = v;
+    __syncthreads();
+    return min(min(reach[0], reach[1]), min(reach[2], reach[3]));
+  };
+  static_assert(NW == 4, "waves");
+  const int quarter = (k + NW - 1) / NW;  // what a quarter of k lanes of each wave reach, k of the workgroup do
 
 #pragma unroll 1
   for (int64_t unit = blockIdx.x; unit < (int64_t)p.n_rows * parts; unit += gridDim.x) {
-    const int64_t row = unit / parts;
+    const int64_t row = parts == 1 ? unit : (int)unit / parts;  // (shared out rows are few)
     const int part = (int)(unit - row * parts);
     const T *z = (const T *)p.logits + row * p.ld;
-    // 16-byte loads, the first of which may begin before the row and the last end behind it
-    const int ahead = (int)((uintptr_t)z / sizeof(T) % E);
-    const int loads = (int)(((int64_t)V + ahead + E - 1) / E);
-    const int each = (loads + parts - 1) / parts;
-    const int64_t l0 = (int64_t)part * each;
-    const int64_t l1 = l0 + each < loads ? l0 + each : loads;
+    // loads of 16 bytes: `loads` of them from element `head` on, single elements before and behind
+    const int head = min(V, (int)(-(uintptr_t)z / sizeof(T) % E)), loads = (V - head) / E;
+    const T *body = z + head;
+    const int l0 = min(loads, part * each), l1 = min(loads, l0 + each);
     Sums sum{-FLT_MAX, 0.f, 0.f};
     int n = 0;             // keys of the list
-    float above = 0.f;     // values that are not at most this one enter it
-    bool begun = false;    // a threshold is there
+    float above = NAN;     // values that are not at most this one enter it
     __syncthreads();       // (the unit before has left LDS)
+    // A key a lane, which enters the list if it is to.
+    auto offer = [&](Key v, bool enters) {
+      uint64_t m = __builtin_amdgcn_ballot_w64(enters);
+      if (!m) return;
+      if (n + __popcll(m) > LIST) {
+        n = keep_largest(list, n, k);
+        above = value((uint32_t)(list[k - 1] >> 32));
+        m = __builtin_amdgcn_ballot_w64(enters && v > list[k - 1]);
+      }
+      if (m >> lane & 1) list[n + bits_below(m)] = v;
+      n += __popcll(m);
+    };
+    u32x4 next[BATCH];
+    auto load = [&](int a) {
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) next[j] = ld16(body + (int64_t)min(a + j * NT + tid, l1 - 1) * E);
+    };
+    if (l0 < l1) load(l0);
 #pragma unroll 1
-    for (int64_t a = l0; a < l1; a += BATCH * NT) {
-      float f[BATCH][E];
+    for (int a = l0; a < l1; a += BATCH * NT) {
+      u32x4 x[BATCH];
 #pragma unroll
       for (int j = 0; j < BATCH; ++j) {
-        const int64_t l = a + j * NT + tid, i = l * E - ahead;
-        if (l < l1 && i >= 0 && i + E <= V) {
-          Elements<T>::get(ld16(z + i), f[j]);
-        } else {
+        const bool mine = a + j * NT + tid < l1;
 #pragma unroll
-          for (int e = 0; e < E; ++e) f[j][e] = l < l1 && i + e >= 0 && i + e < V ? at(z, i + e) : -INFINITY;
-        }
+        for (int i = 0; i < 4; ++i) x[j][i] = mine ? next[j][i] : Elements<T>::NONE;
       }
-      float most = sum.m;
+      if (a + BATCH * NT < l1) load(a + BATCH * NT);
+      float largest[BATCH], most = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j)
+      for (int j = 0; j < BATCH; ++j) {
+        float f[E];
+        Elements<T>::get(x[j], f);
+        largest[j] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < E; ++e) most = fmaxf(most, f[j][e]);
+        for (int e = 0; e < E; ++e) largest[j] = fmaxf(largest[j], f[e]);
+        most = fmaxf(most, largest[j]);
+      }
       if (most > sum.m) sum.to(most);
+      const int steps = (l1 - a - wave * 64 + NT - 1) / NT;  // of the wave that hold anything
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j)
+      for (int j = 0; j < BATCH; ++j) {
+        if (j >= steps) break;
+        float f[E];
+        Elements<T>::get(x[j], f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum.add(f[j][e]);
+        for (int e = 0; e < E; ++e) sum.add(f[e]);
+      }
       if constexpr (TOP) {
-        if (!begun) {  // the k-th largest of the lanes' maxima
-          begun = true;
-          uint32_t own = 0;
-#pragma unroll
-          for (int j = 0; j < BATCH; ++j)
-#pragma unroll
-            for (int e = 0; e < E; ++e) own = max(own, order(f[j][e]));
-          int greater = 0, equal = 0;
-#pragma unroll 4
-          for (int l = 0; l < 64; ++l) {
-            const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)own, l);
-            greater += o > own;
-            equal += o == own;
-          }
-          const uint64_t m = __builtin_amdgcn_ballot_w64(greater < k && greater + equal >= k);
-          uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)own, __builtin_ctzll(m)) - 1;
+        if (a == l0) {  // a value that k of the workgroup's lanes' maxima reach
+          uint32_t o = least_of_waves(reached_by<16>(order(most), quarter)) - 1;
           if (o == 0x7fffffffu) --o;  // (zero's own place below is -0, which equals it)
           above = value(o);
         }
+        // loads that hold something to enter (NaN, which is no maximum, is in the sum) are put
+        // side by side, and their elements offered, one a lane
+        int loads_held = 0;
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
-          uint64_t any = 0;
-#pragma unroll
-          for (int e = 0; e < E; ++e) any |= __builtin_amdgcn_ballot_w64(!(f[j][e] <= above));
-          if (!any) continue;
-          const int64_t i = (a + j * NT + tid) * E - ahead;
-          const bool mine = a + j * NT + tid < l1;
-          auto enters = [&](int e) {
-            return __builtin_amdgcn_ballot_w64(mine && !(f[j][e] <= above) && i + e >= 0 && i + e < V);
-          };
-          int more = 0;
-#pragma unroll
-          for (int e = 0; e < E; ++e) more += __popcll(enters(e));
-          if (n + more > LIST) {
-            n = keep_largest(list, n, k, lane);
-            above = value((uint32_t)(list[k - 1] >> 32));
+          const uint64_t m =
+              __builtin_amdgcn_ballot_w64(a + j * NT + tid < l1 && (!(largest[j] <= above) || sum.s != sum.s));
+          if (!m) continue;
+          if (m >> lane & 1) {
+            held[TOP ? wave : 0][TOP ? loads_held + bits_below(m) : 0] = x[j];
+            held_at[TOP ? wave : 0][TOP ? loads_held + bits_below(m) : 0] = (uint16_t)(j * NT + tid);
           }
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint64_t m = enters(e);
-            if (m >> lane & 1) list[n + bits_below(m)] = key(f[j][e], (int)(i + e));
-            n += __popcll(m);
+          loads_held += __popcll(m);
+        }
+        if (loads_held) {
+          wave_order();
+#pragma unroll 1
+          for (int c = 0; c < loads_held * E; c += 64) {
+            const bool mine = c + lane < loads_held * E;
+            const int h = mine ? (c + lane) / E : 0, e = lane % E;
+            const float v = at((const T *)&held[TOP ? wave : 0][TOP ? h : 0], e);
+            const int i = head + (a + held_at[TOP ? wave : 0][TOP ? h : 0]) * E + e;
+            offer(key(v, i), mine && !(v <= above));
           }
+          wave_order();
         }
       }
+    }
+    // the elements before and behind the loads: at most one a lane
+    if (wave == 0) {
+      const int tail = head + loads * E, i = lane < E ? lane : tail + lane - E;
+      const bool mine = lane < E ? part == 0 && i < head : part == parts - 1 && i < V;
+      const float v = mine ? at(z, i) : -INFINITY;
+      if (v > sum.m) sum.to(v);
+      sum.add(v);
+      if constexpr (TOP) offer(key(v, i), mine && !(v < above));  // (equal ones may lie before those of the list)
     }
     sum.wave();
     if (lane == 0) wave_sums[wave] = sum;
     if constexpr (TOP) {
-      n = keep_largest(list, n, k, lane);
       join_waves(n);
     } else {
       __syncthreads();
@@ -313,14 +407,32 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
         if (last) __hip_atomic_store(&p.tickets[row], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
+      // (the parts are read past the caches, as they were written: no line of them is in one)
       if (!last) continue;
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
       if (TOP) {  // (at most a quarter of LOGP_PARTS parts to a wave)
-        static_assert(LOGP_PARTS / NW * LOGP_MAX_TOP <= LIST, "keys of a quarter of the parts");
-        const int q = (parts + NW - 1) / NW, first = wave * q, count = max(0, min(q, parts - first)) * k;
-        for (int i = lane; i < count; i += 64)
-          list[i] = Part{p, row * parts + first + i / k}.load(2 + i % k);
-        join_waves(keep_largest(list, count, k, lane));
+        const int q = (parts + NW - 1) / NW, first = wave * q, keys_held = max(0, min(q, parts - first)) * k;
+        constexpr int PER = (LOGP_PARTS / NW * LOGP_MAX_TOP + 63) / 64;
+        static_assert(PER * 64 * sizeof(Key) <= BATCH * 64 * sizeof(u32x4), "keys of a quarter of the parts");
+        const Part from{p, row * parts + min(first, parts - 1)};
+        Key keys[PER];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {  // (the quotient of numbers below 2^10 is exact)
+          const int x = max(0, min(i * 64 + lane, keys_held - 1)), part_of = (int)((x + 0.5f) * per_k);
+          keys[i] = from.load(part_of * (2 + LOGP_MAX_TOP) + 2 + x - part_of * k);
+        }
+        lds_key *const mine = (lds_key *)&held[TOP ? wave : 0][0];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          if (i * 64 + lane >= keys_held) keys[i] = 0;
+          most = max(most, (uint32_t)(keys[i] >> 32));
+          mine[i * 64 + lane] = keys[i];
+        }
+        const Key least = (Key)max(1u, least_of_waves(reached_by<32>(most, quarter))) << 32;
+        n = 0;
+#pragma unroll 1
+        for (int c = 0; c < keys_held; c += 64) offer(mine[c + lane], mine[c + lane] >= least);
+        join_waves(n);
       }
       all = Part{p, row * parts + min(lane, parts - 1)}.sums();
       if (lane >= parts) all.s = all.w = 0.f;
@@ -355,15 +467,17 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
 template <typename T>
 hipError_t launch(hipStream_t s, const TokenLogprobs &p) {
   constexpr int E = Elements<T>::N;
-  int64_t parts = (FILL + (int64_t)p.n_rows - 1) / p.n_rows;
-  parts = std::min<int64_t>({parts, LOGP_PARTS, (int64_t)p.vocab / (E * SMALLEST), p.part_floats / 2 / (2 + LOGP_MAX_TOP) / p.n_rows});
-  if (parts < 1 || p.n_rows > p.n_tickets) parts = 1;
-  const int64_t units = parts * p.n_rows;
+  const int64_t loads = (int64_t)p.vocab / E;
+  const int64_t room = p.n_rows <= p.n_tickets ? p.part_floats / 2 / (2 + LOGP_MAX_TOP) / p.n_rows : 1;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({(FILL + p.n_rows - 1) / p.n_rows, LOGP_PARTS, room}));
+  // (whole steps of a workgroup to a part)
+  const int64_t each = std::max<int64_t>(((loads + most - 1) / most + NT - 1) / NT * NT, SMALLEST);
+  const int64_t parts = std::max<int64_t>(1, (loads + each - 1) / each), units = parts * p.n_rows;
   const dim3 grid((unsigned)std::min<int64_t>(units, LOGP_MOST_GROUPS));
   if (p.top > 0)
-    hipLaunchKernelGGL((token_logprobs_kernel<T, true>), grid, dim3(NT), 0, s, p, (int)parts);
+    hipLaunchKernelGGL((token_logprobs_kernel<T, true>), grid, dim3(NT), 0, s, p, (int)parts, (int)each);
   else
-    hipLaunchKernelGGL((token_logprobs_kernel<T, false>), grid, dim3(NT), 0, s, p, (int)parts);
+    hipLaunchKernelGGL((token_logprobs_kernel<T, false>), grid, dim3(NT), 0, s, p, (int)parts, (int)each);
   return hipGetLastError();
 }
 
