@@ -22,7 +22,14 @@ namespace crf {
 namespace {
 
 constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW;
-constexpr int SHORTEST = 4;       // key tiles of a chunk, at least
+// Key tiles of a chunk, at least.  2: two sequences over 8192 24 us instead of 23, eight over
+// 3000 20.8 instead of 19.8 (more parts to join).
+constexpr int SHORTEST = 4;
+// Bytes of K and V that the sequences read by themselves at most, as far as the host can tell,
+// up to which they do.  Shared against by themselves, us: 25 MB (eight sequences over 3000,
+// 12/2 heads) 19.8 / 18.4, 34 MB (two over 8192, 28/4 heads) 23.2 / 21.7, 82 MB (200 over 300,
+// 12/2) 23.5 / 25.9, 135 MB (four over 16384, 28/4) 28.0 / 35.7.
+constexpr int64_t SMALL_READS = 40 << 20;
 constexpr int LONGEST = 1 << 26;  // more than any sequence has
 
 // What the second launch needs of a sequence: its new tokens, and the parts of its own keys and
@@ -85,7 +92,8 @@ struct Groups {
   }
 };
 
-CRF_DEV Item item_of(const SharedAttn &p, const Groups &gr, int i) {
+// Item i; a sequence's tokens are those of seq_new().
+CRF_DEV Item item_of(const SharedAttn &p, const Groups &gr, int i, int row0, int n, int len) {
   Item t{0, 0, 0, 0, 0, -1};
   if (i < gr.n) {
     t.hi = gr.shared[i];
@@ -93,16 +101,20 @@ CRF_DEV Item item_of(const SharedAttn &p, const Groups &gr, int i) {
     t.row0 = gr.row0[i];
     t.n = t.hi > 0 ? gr.rows[i] : 0;
   } else if (i < gr.n + p.a.b.n_seqs) {
-    t.seq = i - gr.n;
-    t.n = seq_new(p.a.b, t.seq, t.row0, t.hi);
-    const int g = t.n > 0 ? gr.of(t.seq) : -1;
+    t = Item{row0, n, 0, len, i - gr.n, -1};
+    const int g = n > 0 ? gr.of(t.seq) : -1;
     // (rows that do not lie among the group's have no part there)
-    if (g >= 0 && gr.shared[g] > 0 && t.row0 >= gr.row0[g] && t.row0 + t.n <= gr.row0[g] + gr.rows[g]) {
+    if (g >= 0 && gr.shared[g] > 0 && row0 >= gr.row0[g] && row0 + n <= gr.row0[g] + gr.rows[g]) {
       t.group = g;
-      t.lo = min(gr.shared[g], t.hi);
+      t.lo = min(gr.shared[g], len);
     }
   }
   return t;
+}
+CRF_DEV Item item_of(const SharedAttn &p, const Groups &gr, int i) {
+  int row0 = 0, n = 0, len = 0;
+  if (i >= gr.n && i < gr.n + p.a.b.n_seqs) n = seq_new(p.a.b, i - gr.n, row0, len);
+  return item_of(p, gr, i, row0, n, len);
 }
 
 // Sums over the workgroup, the same in every thread.
@@ -148,11 +160,12 @@ struct Plan {
     const float k = key_tiles(t), tiles = (float)row_tiles(t) * p.a.nkv, rows = (float)t.n * p.a.nq;
     if (k > 0) sum = make_float4(sum.x + tiles * k, sum.y + tiles, sum.z + rows, sum.w + rows * k);
   }
-  // The chunk's length: units for the workgroups that stay resident, and parts for which there
-  // is room: an item of k tiles has k / c + 1 parts at most.  (Rounded sums: 2^-10 to spare.)
+  // The chunk's length: as many units as half of the workgroups that stay resident (the
+  // sequences' own come on top), and parts for which there is room: an item of k tiles has
+  // k / c + 1 parts at most.  (Rounded sums: 2^-10 to spare.)
   CRF_DEV void choose(float4 sum) {
-    const float room = 0.5f * p.slots, spare = p.part_rows - sum.z * (1.f + 0x1p-10f);
-    float c = fmaxf((float)SHORTEST, ceilf(sum.x / room));
+    const float spare = p.part_rows - sum.z * (1.f + 0x1p-10f);
+    float c = fmaxf((float)SHORTEST, ceilf(sum.x / (0.5f * p.slots)));
     c = fminf(fmaxf(c, ceilf(sum.w / spare * (1.f + 0x1p-10f))), (float)LONGEST);
     chunk = spare > 0 ? (int)c : 0;
     // (sequences or groups that claim the same rows over and over)
@@ -169,14 +182,14 @@ template <typename T, int HD, bool UNI>
 __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p) {
   using L = Layout<T, HD>;
   constexpr int BKV = sizeof(T) == 2 ? 64 : 32, TILE = BKV * L::ROWB;
-  __shared__ __align__(16) char stages[2][2 * TILE];  // the groups while the unit is found; then K, then V
+  __shared__ __align__(16) char stages[2][2 * TILE];  // the groups while a unit is found; then K, then V
   __shared__ int pg[PGCAP];
   __shared__ int token_pos[BM];
   __shared__ float4 sums[NW];
   __shared__ int2 ends[NW];
   __shared__ Unit unit;
   __shared__ int bad;
-  static_assert(Groups::WORDS * 4 <= 4 * TILE, "groups in LDS");
+  static_assert(Groups::WORDS * 4 <= sizeof stages, "groups in LDS");
   const PagedAttn &a = p.a;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -184,16 +197,18 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
   const int G = a.nq / a.nkv;
   const Groups gr((int *)&stages[0][0], p.n_groups);
   const int items = p.n_groups + a.b.n_seqs;
-  const bool one = items <= NT;  // an item to a thread, kept
-  if (tid == 0) {
-    bad = 0;
-    unit.n = 0;
-  }
+  const bool one = items <= NT;  // an item to a thread
+  auto stage_groups = [&] {
+    for (int i = tid; i < p.n_groups; i += NT) gr.stage(p, i);
+    __syncthreads();
+  };
+  int my_row0 = 0, my_n = 0, my_len = 0;  // (the sequence's, while the groups are on their way)
+  if (tid >= p.n_groups && tid < items) my_n = seq_new(a.b, tid - p.n_groups, my_row0, my_len);
+  if (tid == 0) bad = 0;
   if (tid < BM) token_pos[tid] = -1;
-  for (int i = tid; i < p.n_groups; i += NT) gr.stage(p, i);
-  __syncthreads();
+  stage_groups();
   Plan plan{p, BKV, G};
-  Item it = item_of(p, gr, tid);
+  Item it = item_of(p, gr, tid, my_row0, my_n, my_len);
   {
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     plan.add(it, sum);
@@ -201,164 +216,185 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
     for (int i = tid + NT; i < items; i += NT) plan.add(item_of(p, gr, i), sum);
     plan.choose(total(sum, sums));
   }
-  int units = 0, part_rows = 0;  // of the items before
+  // Goes over all items: puts the one that holds unit u into LDS; returns how many units there are.
+  auto scan = [&](int u, bool write) {
+    int units = 0, part_rows = 0;  // of the items before
 #pragma unroll 1
-  for (int i0 = 0; i0 < items; i0 += NT) {
-    if (!one) it = item_of(p, gr, i0 + tid);
-    const int num = plan.row_tiles(it) * plan.tile_units(it), own = it.n * a.nq * plan.chunks(it);
-    int un = num, ro = own;
-    wave_prefix([&](auto c, auto rows) {
-      un += from_lane<c(), rows()>(un);
-      ro += from_lane<c(), rows()>(ro);
-    });
-    if (lane == 63) ends[wave] = make_int2(un, ro);
-    __syncthreads();
-    un += units - num;
-    ro += part_rows - own;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      if (w < wave) un += ends[w].x, ro += ends[w].y;
-      units += ends[w].x;
-      part_rows += ends[w].y;
-    }
-    if ((int)blockIdx.x >= un && (int)blockIdx.x < un + num)
-      unit = Unit{it.row0, it.n, it.lo, it.hi, it.seq, ro, (int)blockIdx.x - un};
-    if (blockIdx.x == 0) {  // (the groups lie before the sequences)
-      const int i = i0 + tid, chunks = plan.chunks(it);
-      if (i < p.n_groups) {
-        gr.base[i] = ro;
-        gr.chunks[i] = chunks;
-      }
+    for (int i0 = 0; i0 < items; i0 += NT) {
+      if (!one) it = item_of(p, gr, i0 + tid);
+      const int num = plan.row_tiles(it) * plan.tile_units(it), own = it.n * a.nq * plan.chunks(it);
+      int from = num, base = own;  // the item's first unit, the first row of its parts
+      wave_prefix([&](auto c, auto rows) {
+        from += from_lane<c(), rows()>(from);
+        base += from_lane<c(), rows()>(base);
+      });
+      __syncthreads();  // (the ends before have been read)
+      if (lane == 63) ends[wave] = make_int2(from, base);
       __syncthreads();
-      if (i >= p.n_groups && i < items) {
-        Info f{{ro, chunks, it.row0, plan.chunk > 0 ? it.n : 0}, {0, 0, 0, 0}};
-        if (it.group >= 0) f.shared = Parts{gr.base[it.group], gr.chunks[it.group], gr.row0[it.group], gr.rows[it.group]};
-        ((Info *)p.info)[i - p.n_groups] = f;
-      }
-    }
-    __syncthreads();
-  }
-  const Unit u{__builtin_amdgcn_readfirstlane(unit.row0), __builtin_amdgcn_readfirstlane(unit.n),
-               __builtin_amdgcn_readfirstlane(unit.lo),   __builtin_amdgcn_readfirstlane(unit.hi),
-               __builtin_amdgcn_readfirstlane(unit.seq),  __builtin_amdgcn_readfirstlane(unit.base),
-               __builtin_amdgcn_readfirstlane(unit.number)};
-  const int n = u.n, lo = u.lo, hi = u.hi;
-  if (n == 0) return;  // more workgroups than units
-  const Item item{u.row0, n, lo, hi, u.seq, -1};
-  const int each = plan.tile_units(item), tile = u.number / each, x = u.number - tile * each;
-  const int chunks = plan.chunks(item), kvh = x / chunks, part = x - kvh * chunks;
-  if (kvh >= a.nkv) return;  // (up to a multiple of 8)
-  const int rows = min(BM, n * G - tile * BM), row0 = tile * BM;
-  const int t0 = plan.first_tile(item) + part * plan.chunk, t1 = min(t0 + plan.chunk, (hi + BKV - 1) / BKV);
-  const int first = u.row0 + row0 / G, tokens = (row0 + rows - 1) / G - row0 / G + 1;  // of the tile
-
-  // positions of the tile's tokens (-1: of no sequence)
-  auto place = [&](int start, int m, int len) {
-    for (int t = max(start, first); t < min(start + m, first + tokens); ++t) token_pos[t - first] = len - m + t - start;
-  };
-  if (one) {
-    if (tid >= p.n_groups && it.n > 0) place(it.row0, it.n, it.hi);
-  } else {
-    for (int s = u.seq + tid; s < a.b.n_seqs; s += NT) {
-      int start, len;
-      const int m = seq_new(a.b, s, start, len);
-      if (start >= first + tokens) break;
-      place(start, m, len);
-    }
-  }
-  Pages<T, HD, UNI, BKV / NW> pages{a.b, a.zeros, pg, &bad, 0, hi, kvh, wave * (BKV / NW), lane,
-                                    a.b.tables + (int64_t)u.seq * a.b.table_stride};
-  const int end_key = t1 * BKV;
-  pages.fill(div_by(t0 * BKV, a.b.ps_div), end_key, NT);
-  // this lane's row (padding rows repeat the last one)
-  const int r = wave * 32 + l32, row = row0 + min(r, rows - 1);
-  const int tok = row / G, head = kvh * G + row - tok * G;
-  QFrag<T, HD> q;
-  q.load((const T *)a.q + (int64_t)(u.row0 + tok) * a.q_ld + head * HD, g);
-  RowState<HD> st;
-  __syncthreads();
-  const int last_key = min(token_pos[u.row0 + tok - first], hi - 1);  // of those that the row sees
-  int least = last_key, most = last_key;
+      from += units - num;
+      base += part_rows - own;
 #pragma unroll
-  for (int o = 16; o >= 1; o /= 2) {
-    least = min(least, __shfl_xor(least, o, 64));
-    most = max(most, __shfl_xor(most, o, 64));
-  }
-  least = __builtin_amdgcn_readfirstlane(least);
-  most = __builtin_amdgcn_readfirstlane(most);
-  const int whole_to = wave * 32 < rows ? least + 1 : 0;  // keys before it are seen by every row of the wave
-  bool careful = false, strictly = false;
-  uint64_t strict = 0;
-#pragma unroll 1
-  for (;;) {
-    st.clear();
-    const lds_mem *mem = (const lds_mem *)&stages[0][0];
-    auto load = [&](int i, int stage) {
-      const lds_mem *k = mem + stage * 2 * TILE;
-      pages.load(i * BKV + wave * (BKV / NW), k, k + TILE);
-    };
-    load(t0, 0);
-    // A tile's data is there, the next one's is on its way (each wave passes here once a
-    // tile, wherever it then goes).
-    auto arrive = [&](int i) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (i + 1 < t1) {
-        if (div_by(min((i + 2) * BKV, hi) - 1, a.b.ps_div) >= pages.first + PGCAP) {
-          pages.fill(div_by(i * BKV, a.b.ps_div), end_key, NT);
-          __syncthreads();
+      for (int w = 0; w < NW; ++w) {
+        if (w < wave) from += ends[w].x, base += ends[w].y;
+        units += ends[w].x;
+        part_rows += ends[w].y;
+      }
+      if (u >= from && u < from + num) unit = Unit{it.row0, it.n, it.lo, it.hi, it.seq, base, u - from};
+      if (write) {  // (the groups lie before the sequences)
+        const int i = i0 + tid, chunks = plan.chunks(it);
+        if (i < p.n_groups) {
+          gr.base[i] = base;
+          gr.chunks[i] = chunks;
         }
-        load(i + 1, (i + 1 - t0) & 1);
+        __syncthreads();
+        if (i >= p.n_groups && i < items) {
+          Info f{{base, chunks, it.row0, plan.chunk > 0 ? it.n : 0}, {0, 0, 0, 0}};
+          if (it.group >= 0)
+            f.shared = Parts{gr.base[it.group], gr.chunks[it.group], gr.row0[it.group], gr.rows[it.group]};
+          ((Info *)p.info)[i - p.n_groups] = f;
+        }
       }
-    };
-    q.arrived();
-#pragma unroll 1
-    for (int i = t0; i < t1;) {
-      int taken = 0;  // blocks of the tile
-      for (;;) {
-        arrive(i);
-        const int kt0 = i * BKV;
-        if (i == t0 || kt0 + BKV > whole_to || kt0 < lo || bad || careful) break;
-        const lds_mem *kt = mem + ((i - t0) & 1) * 2 * TILE;
-        taken = whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, a.scale_log2, lane);
-        if (taken < BKV / 32) break;
-        taken = 0;
-        if (++i == t1) break;
-      }
-      if (i == t1) break;
-      const int kt0 = i * BKV;
-      if (wave * 32 < rows && kt0 <= most && kt0 + BKV > lo) {
-        const Seen<false> seen{lo, last_key, lo, whole_to, hi, bad != 0, pg, pages.first, a.b.ps_div, strict, 0};
-        const lds_mem *kt = mem + ((i - t0) & 1) * 2 * TILE;
-#pragma unroll 1
-        for (int kb = 32 * taken; kb < BKV; kb += 32)
-          if (careful)
-            block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, a.scale_log2, lane,
-                                  seen);
-          else
-            block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, a.scale_log2, lane, seen);
-      }
-      ++i;
     }
-    const uint64_t odd = not_finite(st);
-    const bool again = __syncthreads_or(odd != 0);
-    if (strictly || !again) break;
-    if (careful) strict = odd;
-    strictly = careful;
-    careful = true;
-    pages.fill(div_by(t0 * BKV, a.b.ps_div), end_key, NT);
+    return units;
+  };
+  const int units = scan((int)blockIdx.x, blockIdx.x == 0);
+  // The units, of which the first (the groups') are the longest, are dealt out back and forth.
+#pragma unroll 1
+  for (int round = 0;; ++round) {
+    const int nth = round * (int)gridDim.x + (round % 2 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    if (nth >= units) break;
+    if (round > 0) {  // (the items are worked out again: kept, their registers would be spilled)
+      __syncthreads();  // (the unit before has left LDS)
+      stage_groups();
+      it = item_of(p, gr, tid);
+      scan(nth, false);
+      if (tid == 0) bad = 0;
+      if (tid < BM) token_pos[tid] = -1;
+    }
     __syncthreads();
-  }
+    const Unit u{__builtin_amdgcn_readfirstlane(unit.row0), __builtin_amdgcn_readfirstlane(unit.n),
+                 __builtin_amdgcn_readfirstlane(unit.lo),   __builtin_amdgcn_readfirstlane(unit.hi),
+                 __builtin_amdgcn_readfirstlane(unit.seq),  __builtin_amdgcn_readfirstlane(unit.base),
+                 __builtin_amdgcn_readfirstlane(unit.number)};
+    const int n = u.n, lo = u.lo, hi = u.hi;
+    const Item item{u.row0, n, lo, hi, u.seq, -1};
+    const int each = plan.tile_units(item), tile = u.number / each, x = u.number - tile * each;
+    const int chunks = plan.chunks(item), kvh = x / chunks, part = x - kvh * chunks;
+    if (kvh >= a.nkv) continue;  // (up to a multiple of 8)
+    const int rows = min(BM, n * G - tile * BM), row0 = tile * BM;
+    const int t0 = plan.first_tile(item) + part * plan.chunk, t1 = min(t0 + plan.chunk, (hi + BKV - 1) / BKV);
+    const int first = u.row0 + row0 / G, tokens = (row0 + rows - 1) / G - row0 / G + 1;  // of the tile
 
-  const float l = st.l + __shfl_xor(st.l, 32, 64);
-  if (r < rows) {
-    const int64_t slot = u.base + ((int64_t)part * a.nkv + kvh) * n * G + row0 + r;
-    float *o = p.o + slot * HD + 4 * g;
+    // this lane's row (padding rows repeat the last one)
+    const int r = wave * 32 + l32, row = row0 + min(r, rows - 1);
+    const int tok = row / G, head = kvh * G + row - tok * G;
+    QFrag<T, HD> q;
+    q.load((const T *)a.q + (int64_t)(u.row0 + tok) * a.q_ld + head * HD, g);
+    // positions of the tile's tokens (-1: of no sequence)
+    auto place = [&](int start, int m, int len) {
+      for (int t = max(start, first); t < min(start + m, first + tokens); ++t)
+        token_pos[t - first] = len - m + t - start;
+    };
+    if (one) {
+      if (tid >= p.n_groups && it.n > 0) place(it.row0, it.n, it.hi);
+    } else {
+      for (int s = u.seq + tid; s < a.b.n_seqs; s += NT) {
+        int start, len;
+        const int m = seq_new(a.b, s, start, len);
+        if (start >= first + tokens) break;
+        place(start, m, len);
+      }
+    }
+    Pages<T, HD, UNI, BKV / NW> pages{a.b, a.zeros, pg, &bad, 0, hi, kvh, wave * (BKV / NW), lane,
+                                      a.b.tables + (int64_t)u.seq * a.b.table_stride};
+    const int end_key = t1 * BKV;
+    pages.fill(div_by(t0 * BKV, a.b.ps_div), end_key, NT);
+    RowState<HD> st;
+    __syncthreads();
+    const int last_key = min(token_pos[u.row0 + tok - first], hi - 1);  // of those that the row sees
+    int least = last_key, most = last_key;
 #pragma unroll
-    for (int i = 0; i < 4 * L::HB; ++i)
-      *(f32x4 *)(o + 8 * i) = f32x4{st.o[i / 4][4 * (i % 4)], st.o[i / 4][4 * (i % 4) + 1], st.o[i / 4][4 * (i % 4) + 2],
-                                    st.o[i / 4][4 * (i % 4) + 3]};
-    if (g == 0) p.ml[slot] = make_float2(st.ref, l);
+    for (int o = 16; o >= 1; o /= 2) {
+      least = min(least, __shfl_xor(least, o, 64));
+      most = max(most, __shfl_xor(most, o, 64));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+    const int whole_to = wave * 32 < rows ? least + 1 : 0;  // keys before it are seen by every row of the wave
+    bool careful = false, strictly = false;
+    uint64_t strict = 0;
+#pragma unroll 1
+    for (;;) {
+      st.clear();
+      const lds_mem *mem = (const lds_mem *)&stages[0][0];
+      auto load = [&](int i) {
+        const lds_mem *k = mem + ((i - t0) & 1) * 2 * TILE;
+        pages.load(i * BKV + wave * (BKV / NW), k, k + TILE);
+      };
+      load(t0);
+      // A tile's data is there, the next one's is on its way (each wave passes here once a
+      // tile, wherever it then goes).
+      auto arrive = [&](int i) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (i + 1 < t1) {
+          if (div_by(min((i + 2) * BKV, hi) - 1, a.b.ps_div) >= pages.first + PGCAP) {
+            pages.fill(div_by(i * BKV, a.b.ps_div), end_key, NT);
+            __syncthreads();
+          }
+          load(i + 1);
+        }
+      };
+      q.arrived();
+#pragma unroll 1
+      for (int i = t0; i < t1;) {
+        int taken = 0;  // blocks of the tile
+        for (;;) {
+          arrive(i);
+          const int kt0 = i * BKV;
+          if (i == t0 || kt0 + BKV > whole_to || kt0 < lo || bad || careful) break;
+          const lds_mem *kt = mem + ((i - t0) & 1) * 2 * TILE;
+          taken = whole_blocks<T, HD, BKV / 32>(kt, kt + TILE, q, st, a.scale_log2, lane);
+          if (taken < BKV / 32) break;
+          taken = 0;
+          if (++i == t1) break;
+        }
+        if (i == t1) break;
+        const int kt0 = i * BKV;
+        if (wave * 32 < rows && kt0 <= most && kt0 + BKV > lo) {
+          const Seen<false> seen{lo, last_key, lo, whole_to, hi, bad != 0, pg, pages.first, a.b.ps_div, strict, 0};
+          const lds_mem *kt = mem + ((i - t0) & 1) * 2 * TILE;
+#pragma unroll 1
+          for (int kb = 32 * taken; kb < BKV; kb += 32)
+            if (careful)
+              block<T, HD, CAREFUL>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, a.scale_log2, lane,
+                                    seen);
+            else
+              block<T, HD, SOME>(kt + kb * L::ROWB, kt + TILE + kb * L::ROWB, kt0 + kb, q, st, a.scale_log2, lane,
+                                 seen);
+        }
+        ++i;
+      }
+      const uint64_t odd = not_finite(st);
+      const bool again = __syncthreads_or(odd != 0);
+      if (strictly || !again) break;
+      if (careful) strict = odd;
+      strictly = careful;
+      careful = true;
+      pages.fill(div_by(t0 * BKV, a.b.ps_div), end_key, NT);
+      __syncthreads();
+    }
+
+    const float l = st.l + __shfl_xor(st.l, 32, 64);
+    if (r < rows) {
+      const int64_t slot = u.base + ((int64_t)part * a.nkv + kvh) * n * G + row0 + r;
+      float *o = p.o + slot * HD + 4 * g;
+#pragma unroll
+      for (int i = 0; i < 4 * L::HB; ++i)
+        *(f32x4 *)(o + 8 * i) = f32x4{st.o[i / 4][4 * (i % 4)], st.o[i / 4][4 * (i % 4) + 1],
+                                      st.o[i / 4][4 * (i % 4) + 2], st.o[i / 4][4 * (i % 4) + 3]};
+      if (g == 0) p.ml[slot] = make_float2(st.ref, l);
+    }
   }
 }
 
@@ -391,14 +427,7 @@ __global__ __launch_bounds__(NT) void shared_join_kernel(const SharedAttn p) {
         const int c = s ? j : j - f.shared.chunks;
         return (int64_t)q.base + ((int64_t)c * a.nkv + kvh) * q.n * G + (token - q.row0) * G + r;
       };
-      float top = -INFINITY;
-      for (int j = tid % LANES; j < parts; j += LANES) {
-        const float2 m = p.ml[slot(j)];
-        if (m.y != 0.f) top = fmaxf(top, m.x);
-      }
-#pragma unroll
-      for (int o = LANES / 2; o >= 1; o /= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
-      float l = 0.f;
+      float top = -INFINITY, l = 0.f;
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
       // (a part of which the row sees nothing weighs nothing)
       constexpr int U = 8;
@@ -412,9 +441,21 @@ __global__ __launch_bounds__(NT) void shared_join_kernel(const SharedAttn p) {
           m[u] = p.ml[at];
           x[u] = *(const f32x4 *)(p.o + at * HD + e);
         }
+        float most = top;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (j0 + u >= parts || m[u].y == 0.f) continue;
+          if (j0 + u >= parts) m[u].y = 0.f;
+          if (m[u].y != 0.f) most = fmaxf(most, m[u].x);
+        }
+        if (l != 0.f) {
+          const float w = rescale(top, most);
+          l *= w;
+          sum *= w;
+        }
+        top = most;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (m[u].y == 0.f) continue;
           const float w = rescale(m[u].x, top);
           l = fmaf(w, m[u].y, l);
 #pragma unroll
@@ -438,13 +479,7 @@ __global__ __launch_bounds__(NT) void shared_join_kernel(const SharedAttn p) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const SharedAttn &p) {
   const PagedBatch &b = p.a.b;
-  const int G = p.a.nq / p.a.nkv;
-  // units: as many as the chunk is chosen for, one more to each row tile and KV head of an item
-  // (whose last tile may be short), and up to 7 more to each row tile of items of several
-  const int64_t tiles = 2 * ((int64_t)b.n_rows * G / BM) + p.n_groups + b.n_seqs;
-  const int64_t most = 2 * (int64_t)p.slots + tiles * p.a.nkv + 7 * tiles;
-  if (most > MOST_GROUPS) return hipErrorInvalidConfiguration;  // (more rows than the parts' room is for)
-  const dim3 grid((unsigned)most);
+  const dim3 grid((unsigned)p.slots);
   if (b.page_size % 16 == 0)
     hipLaunchKernelGGL((shared_parts_kernel<T, HD, true>), grid, dim3(NT), 0, s, p);
   else
@@ -465,9 +500,12 @@ hipError_t launch_shared_attn(hipStream_t s, bool f32, SharedAttn p) {
   const int64_t table = (int64_t)b.n_seqs * (int64_t)(sizeof(Info) / 4);
   const int64_t rows = (p.a.part_floats - table) / (p.a.hd + 2);
   p.part_rows = rows < INT32_MAX ? (int)rows : INT32_MAX;
-  // Without a group, where a sequence fills a tile by itself, or without room for four parts
-  // of every row, each sequence reads its shared keys itself.
-  if (p.n_groups == 0 || p.n_groups > SHARED_MAX_GROUPS || (int64_t)b.max_new * G > BM ||
+  // Without a group, where a sequence fills a tile by itself, where all that the sequences read
+  // by themselves is little, or without room for four parts of every row, each sequence reads
+  // its shared keys itself.
+  const int64_t reads = (int64_t)b.n_seqs * std::min<int64_t>((int64_t)b.max_pages * b.page_size, (int64_t)1 << 24) *
+                        p.a.nkv * p.a.hd * (f32 ? 8 : 4);
+  if (p.n_groups == 0 || p.n_groups > SHARED_MAX_GROUPS || (int64_t)b.max_new * G > BM || reads <= SMALL_READS ||
       rows < 4 * (int64_t)b.n_rows * p.a.nq)
     return launch_paged_attn(s, f32, p.a);
   p.info = p.a.part;

@@ -17,9 +17,10 @@ def _i32(v):
 
 class Grouped:
     """groups: (shared tokens, [(new, own cached) ...]); alone: (new, cached) behind them.  A Batch whose group members'
-    first pages are the first member's (a begun page is a copy, as a fork leaves it)."""
+    first pages are the first member's (a begun page is a copy, as a fork leaves it).  Tables are as wide as it takes
+    for the batch not to count as a small one, whose sequences read their keys by themselves (small: as they are)."""
 
-    def __new__(cls, groups, nq, nkv, hd, dtype, alone=(), page=16, seed=0, pad=0, max_new=None, ahead=()):
+    def __new__(cls, groups, nq, nkv, hd, dtype, alone=(), page=16, seed=0, pad=0, max_new=None, ahead=(), small=False):
         import paper_2609_30884_amd as crf
         from tests.paged import Batch
         seqs, start, shared = list(ahead), [len(ahead)], []
@@ -27,7 +28,10 @@ class Grouped:
             seqs += [(n, doc + own) for n, own in members]
             start.append(len(seqs))
             shared.append(doc)
-        b = Batch(seqs + list(alone), nq, nkv, hd, dtype, page=page, seed=seed, pad=pad, max_new=max_new)
+        seqs += list(alone)
+        one = page * nkv * hd * 2 * (2 if dtype == BF else 4)  # bytes of a page
+        wide = 0 if small else (41 << 20) // (one * len(seqs)) + 1
+        b = Batch(seqs, nq, nkv, hd, dtype, page=page, seed=seed, pad=pad, max_new=max_new, wide=wide)
         for g, doc in enumerate(shared):
             first = start[g]
             for s in range(first + 1, start[g + 1]):
@@ -114,18 +118,21 @@ def test_many_groups_and_sequences():
     _check(Grouped([(20, [(1, i % 7)]) for i in range(1100)], 2, 2, 64, BF, seed=9), "more groups than are shared")
 
 
-def test_chunks_take_the_plain_kernels():
-    """Sequences that fill tiles by themselves, and a batch whose parts the workspace does not hold."""
+def test_what_the_plain_kernels_take():
+    """Small batches, sequences that fill tiles by themselves, and a batch whose parts the workspace does not hold."""
     import paper_2609_30884_amd as crf
     from tests.paged import context
     print("[case] shared chunks", flush=True)
-    b = Grouped([(300, [(70, 20), (200, 0)])], 12, 2, 64, BF, seed=11)
     ctx = context(12, 2, 64, BF)
-    out, _, _ = _check(b, "chunks", ctx=ctx)
-    want = torch.zeros_like(out)
-    crf.paged_attention(ctx, b.batch, b.q, b.pool, 1, want)
-    torch.cuda.synchronize()
-    assert torch.equal(out, want)
+    for what, b in (("small", Grouped([(300, [(1, 20), (2, 0)])], 12, 2, 64, BF, seed=11, small=True)),
+                    ("chunks", Grouped([(300, [(70, 20), (200, 0)])], 12, 2, 64, BF, seed=11))):
+        out, _, _ = _check(b, what, ctx=ctx)
+        want = torch.zeros_like(out)
+        crf.paged_attention(ctx, b.batch, b.q, b.pool, 1, want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    b = Grouped([(300, [(1, 20), (2, 0)])], 12, 2, 64, BF, seed=11)
+    assert not torch.equal(_check(b, "shared", ctx=ctx)[0], torch.zeros_like(b.q))
     b = Grouped([(30, [(9, 0)] * 900)], 28, 4, 128, BF, seed=11)  # 226800 rows of heads
     _check(b, "no room", ctx=context(28, 4, 128, BF))
 
@@ -170,7 +177,7 @@ def test_rows_claimed_over_and_over():
     ctx, n = context(28, 4, 128, BF), 2600
     guard = torch.full((b.n_rows + 8, 28, 128), 7.0, dtype=BF, device="cuda")
     back = _i32([4 * (i % 2) for i in range(n + 1)])
-    batch = crf.seq_batch(back, b.length[:1].repeat(n), b.tables[:1].repeat(n, 1), b.n_rows, 4)
+    batch = crf.seq_batch(back, b.length[:1].repeat(n), b.tables[:1, :40].repeat(n, 1), b.n_rows, 4)
     crf.shared_attention(ctx, batch, b.groups, b.q, b.pool, 1, guard[4:-4])
     torch.cuda.synchronize()
     assert ctx.device_errors() == 2
