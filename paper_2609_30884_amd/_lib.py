@@ -454,10 +454,11 @@ def _storage(dims: ModelDims):
     return torch.bfloat16 if dims.dtype == CRF_BF16 else torch.float32
 
 
-def _head_rows(d: ModelDims, t, n_rows: int, heads: int, name: str):
-    """Pointer and row stride of [rows, heads, head_dim] or [rows, heads * head_dim] whose rows are contiguous."""
+def _head_rows(d: ModelDims, t, n_rows: int, heads: int, name: str, dtype=None):
+    """Pointer and row stride of [rows, heads, head_dim] or [rows, heads * head_dim] whose rows are contiguous (dtype: the
+    context's storage type, where the caller has it)."""
     shape, stride, hd = t.shape, t.stride(), d.head_dim
-    if t.dtype is not _storage(d):
+    if t.dtype is not (dtype or _storage(d)):
         raise CrfError(1, f"{name} is {t.dtype}, the context's storage type differs")
     if len(shape) == 3:
         ok = shape[1] == heads and shape[2] == hd and (heads == 1 or stride[1] == hd)
@@ -517,12 +518,12 @@ def _append_rows(ctx: Context, batch: SeqBatch, q, k, v, pool: PagePool, layer: 
     """Checks of an append's tensors; positions and the pointer and row stride of q, k, v and q_out."""
     d, n = ctx.dims, batch.n_rows
     _check_pool(ctx.dims, pool, layer + 1)
-    qp, qs = _head_rows(d, q, n, d.n_q_heads, "q") if q is not None else (None, 0)
-    op, os_ = _head_rows(d, q_out, n, d.n_q_heads, "q_out") if q_out is not None else (None, 0)
-    kp, ks = _head_rows(d, k, n, d.n_kv_heads, "k")
-    vp, vs = _head_rows(d, v, n, d.n_kv_heads, "v")
+    dt, nq, nkv = pool.tensors[0].dtype, d.n_q_heads, d.n_kv_heads
+    qp, qs = _head_rows(d, q, n, nq, "q", dt) if q is not None else (None, 0)
+    op, os_ = _head_rows(d, q_out, n, nq, "q_out", dt) if q_out is not None else (None, 0)
+    kp, ks = _head_rows(d, k, n, nkv, "k", dt)
+    vp, vs = _head_rows(d, v, n, nkv, "v", dt)
     pp = _int32(positions, n, "positions").data_ptr() if positions is not None else None
-    _check_device(ctx, (batch, pool), (q, k, v, q_out, positions))
     return pp, (qp, qs, kp, ks, vp, vs), (op, os_)
 
 
@@ -530,13 +531,16 @@ def rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, pool: PagePo
                 positions=None, stream=None):
     """crf_rope_append: q rotated into q_out (both None: keys and values only), k rotated and v into the pages."""
     pp, rows, out = _append_rows(ctx, batch, q, k, v, pool, layer, q_out, positions)
+    _check_device(ctx, (batch, pool), (q, k, v, q_out, positions))
     st = ctx.lib.crf_rope_append(ctx.handle, rope, batch, pp, *rows, *out, pool, layer, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 
-def _gain(d: ModelDims, t, name: str):
-    """Pointer of a head's gains [head_dim] in the storage type."""
-    if t.dtype is not _storage(d):
+def _gain(d: ModelDims, t, name: str, dtype):
+    """Pointer of a head's gains [head_dim] in the storage type (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
         raise CrfError(1, f"{name} is {t.dtype}, the context's storage type differs")
     if t.shape != (d.head_dim,) or not t.is_contiguous():
         raise CrfError(2, f"{name} must be a contiguous vector of {d.head_dim}")
@@ -548,9 +552,10 @@ def norm_rope_append(ctx: Context, rope: Rope, batch: SeqBatch, q, k, v, q_norm,
     """crf_norm_rope_append: rope_append of q and k whose heads are normed first, with gains q_norm and k_norm
     [head_dim] (q, q_norm and q_out None: keys and values only)."""
     pp, rows, out = _append_rows(ctx, batch, q, k, v, pool, layer, q_out, positions)
-    gains = [None if g is None else _gain(ctx.dims, g, name) for g, name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
-    _check_device(ctx, (), (q_norm, k_norm))
-    st = ctx.lib.crf_norm_rope_append(ctx.handle, rope, batch, pp, *rows, *gains, *out, pool, layer, _stream(stream))
+    dt = pool.tensors[0].dtype
+    qn, kn = _gain(ctx.dims, q_norm, "q_norm", dt), _gain(ctx.dims, k_norm, "k_norm", dt)
+    _check_device(ctx, (batch, pool), (q, k, v, q_out, positions, q_norm, k_norm))
+    st = ctx.lib.crf_norm_rope_append(ctx.handle, rope, batch, pp, *rows, qn, kn, *out, pool, layer, _stream(stream))
     _err(ctx.lib, ctx.handle, st)
 
 
@@ -558,10 +563,11 @@ def _attention_rows(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int
     """Checks of attention's tensors; pointer and row stride of q and out."""
     d, n = ctx.dims, batch.n_rows
     _check_pool(ctx.dims, pool, layer + 1)
-    rows = _head_rows(d, q, n, d.n_q_heads, "q"), _head_rows(d, out, n, d.n_q_heads, "out")
+    dt, nq = pool.tensors[0].dtype, d.n_q_heads
+    rows = _head_rows(d, q, n, nq, "q", dt), _head_rows(d, out, n, nq, "out", dt)
     if lse is not None:
-        if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, d.n_q_heads) or not lse.is_contiguous():
-            raise CrfError(2, f"lse must be contiguous float32 [{n}, {d.n_q_heads}]")
+        if not lse.is_floating_point() or lse.element_size() != 4 or lse.shape != (n, nq) or not lse.is_contiguous():
+            raise CrfError(2, f"lse must be contiguous float32 [{n}, {nq}]")
     _check_device(ctx, (batch, pool), (q, out, lse))
     return rows
 
@@ -694,21 +700,22 @@ def token_logprobs(ctx: Context, logits, tokens=None, logprob=None, entropy=None
     rows, vocab = logits.shape
     if (tokens is None) != (logprob is None) or (top_token is None) != (top_logprob is None):
         raise CrfError(1, "tokens and logprob, top_token and top_logprob are given together or not at all")
-    n = top = 0
-    if tokens is not None:
-        if tokens.dim() not in (1, 2) or tokens.shape[0] != rows:
-            raise CrfError(2, f"tokens {tuple(tokens.shape)} are not those of {rows} rows")
-        n = 1 if tokens.dim() == 1 else tokens.shape[1]
-    if top_token is not None:
-        if top_token.dim() != 2:
-            raise CrfError(2, "top_token must be [rows, top]")
-        top = top_token.shape[1]
     f32, i32 = torch.float32, torch.int32
-    tp = _values(tokens, tokens.shape if n else None, i32, "tokens") if n else None
-    lp = _values(logprob, tokens.shape, f32, "logprob") if n else None
+    n = top = 0
+    tp = lp = kp = vp = None
+    if tokens is not None:
+        shape = tokens.shape
+        if len(shape) not in (1, 2) or shape[0] != rows:
+            raise CrfError(2, f"tokens {tuple(shape)} are not those of {rows} rows")
+        n = 1 if len(shape) == 1 else shape[1]
+        tp, lp = _values(tokens, shape, i32, "tokens"), _values(logprob, shape, f32, "logprob")
+    if top_token is not None:
+        shape = top_token.shape
+        if len(shape) != 2 or shape[0] != rows:
+            raise CrfError(2, f"top_token must be [{rows}, top]")
+        top = shape[1]
+        kp, vp = _values(top_token, shape, i32, "top_token"), _values(top_logprob, shape, f32, "top_logprob")
     ep, sp = _values(entropy, (rows,), f32, "entropy"), _values(lse, (rows,), f32, "lse")
-    kp = _values(top_token, (rows, top), i32, "top_token") if top else None
-    vp = _values(top_logprob, (rows, top), f32, "top_logprob") if top else None
     _check_device(ctx, (), (logits, tokens, logprob, entropy, lse, top_token, top_logprob))
     st = ctx.lib.crf_token_logprobs(ctx.handle, CRF_F32 if logits.dtype is f32 else CRF_BF16, logits.data_ptr(),
                                     logits.stride(0) if rows > 1 else vocab, rows, vocab, tp, n, lp, ep, sp, top, kp, vp,

@@ -55,16 +55,27 @@ struct Vec<float> {
   }
 };
 
-// The squares of the N values f of each of a head's n lanes (a power of two, neighbours),
-// to the factor that makes their root mean square one.
+// The sum over n neighbouring lanes (4, 8 or 16, all or none of them active), in each.
+CRF_DEV float lanes_sum(float v, int n) {
+  auto from = [&](auto c) {
+    return __builtin_bit_cast(float,
+                              __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), c(), 0xf, 0xf, true));
+  };
+  v += from(std::integral_constant<int, 0xb1>());                // quad_perm [1, 0, 3, 2]
+  v += from(std::integral_constant<int, 0x4e>());                // quad_perm [2, 3, 0, 1]
+  if (n > 4) v += from(std::integral_constant<int, 0x141>());    // row_half_mirror
+  if (n > 8) v += from(std::integral_constant<int, 0x140>());    // row_mirror
+  return v;
+}
+// The factor that makes the root mean square of a head one, whose values are the N of each of n
+// lanes.
 template <int N>
 CRF_DEV float unit_rms(float (&f)[N], int n, float mean, float eps) {
   auto squares = [&] {
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) ss = fmaf(f[i], f[i], ss);
-    for (int o = n / 2; o >= 1; o /= 2) ss += __shfl_xor(ss, o, 64);
-    return ss;
+    return lanes_sum(ss, n);
   };
   float ss = squares();
   if (ss == INFINITY) {  // (values past 2^63: again with smaller ones, next to which eps is nothing)
@@ -81,8 +92,14 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
   constexpr int E = Vec<T>::E;
   __shared__ int pos_s[TPW], page_s[TPW], slot_s[TPW], seq_s[TPW];
   __shared__ float cs[TPW][64], sn[TPW][64];
+  __shared__ __align__(16) T gains[2][NORM ? 128 : 1];  // of q and of k
   const PagedBatch &b = p.b;
   const int tid = threadIdx.x;
+  if constexpr (NORM)  // (seen by all from the first barrier on)
+    for (int i = tid; i < 2 * p.hd; i += NT) {
+      const T *g = (const T *)(i < p.hd ? p.q_norm : p.k_norm);
+      if (g) gains[i / p.hd][i % p.hd] = g[i % p.hd];
+    }
 #pragma unroll 1
   for (int64_t first = (int64_t)blockIdx.x * TPW; first < b.n_rows; first += (int64_t)gridDim.x * TPW) {
     const int row0 = (int)first;
@@ -127,12 +144,14 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
 
     const int upr = half / E;                     // rotated units of a head
     const int uph = p.hd / (2 * E);               // units of a head
-    const int heads = p.nq + 2 * p.nkv, items = heads * uph;
-    for (int x = tid; x < TPW * items; x += NT) {
-      const int j = TPW == 1 ? 0 : x / items, i = TPW == 1 ? x : x % items;
+    // (uph is 4, 8 or 16: a thread has the same unit of all its heads)
+    const int u = tid % uph, step = NT / uph, heads = p.nq + 2 * p.nkv;
+    int j = 0;  // the token, of which the thread's head is h
+    for (int h = tid / uph;; h += step) {
+      while (h >= heads) h -= heads, ++j;
+      if (j >= TPW) break;
       if (pos_s[j] < 0) continue;
       const int64_t row = row0 + j;
-      const int h = i / uph, u = i % uph;
       const T *src;
       T *dst;
       const bool is_q = h < p.nq, is_v = h >= p.nq + p.nkv;
@@ -160,7 +179,7 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
         Vec<T>::unpack(a, f);
         Vec<T>::unpack(c, f + E);
         if constexpr (NORM) {
-          const T *gain = (const T *)(is_q ? p.q_norm : p.k_norm);
+          const T *gain = gains[is_q ? 0 : 1];
           Vec<T>::unpack(ld16(gain + o0), g);
           Vec<T>::unpack(ld16(gain + o1), g + E);
           const float r = unit_rms(f, uph, 1.f / p.hd, p.eps);
