@@ -77,14 +77,17 @@ CRF_DEV float unit_rms(float (&f)[N], int n, float mean, float eps) {
     for (int i = 0; i < N; ++i) ss = fmaf(f[i], f[i], ss);
     return lanes_sum(ss, n);
   };
-  float ss = squares();
-  if (ss == INFINITY) {  // (values past 2^63: again with smaller ones, next to which eps is nothing)
+  float ss = squares(), sq = fmaf(ss, mean, eps);
+  if (ss == INFINITY || sq < 0x1p-80f) {
+    // squares that pass the range of fp32 at either end: again with values scaled by 2^-80 (eps
+    // is nothing next to them), or, where eps does not outweigh them, by 2^80
+    const bool large = ss == INFINITY;
+    const float scale = large ? 0x1p-80f : 0x1p80f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] *= 0x1p-80f;
-    ss = squares();
-    eps = 0.f;
+    for (int i = 0; i < N; ++i) f[i] *= scale;
+    sq = fmaf(squares(), mean, large ? 0.f : eps * 0x1p80f * 0x1p80f);
   }
-  return rsqrtf(fmaf(ss, mean, eps));
+  return rsqrtf(sq);
 }
 
 template <typename T, int TPW, bool NORM>

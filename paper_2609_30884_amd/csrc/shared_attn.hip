@@ -139,15 +139,16 @@ CRF_DEV float4 total(float4 v, float4 *lds) {
 // The units of an item: its chunks and KV heads, row tile after row tile; where there are several
 // tiles, each tile's begin at a multiple of 8, so that those that share keys lie on one XCD
 // (blockIdx.x % 8).
+template <int BKV>
 struct Plan {
   const SharedAttn &p;
-  int bkv, G;
+  int G;
   int chunk = 0;  // key tiles of a unit (0: no item is computed)
 
   CRF_DEV int row_tiles(const Item &t) const { return (t.n * G + BM - 1) / BM; }
-  CRF_DEV int first_tile(const Item &t) const { return t.lo / bkv; }
+  CRF_DEV int first_tile(const Item &t) const { return t.lo / BKV; }
   CRF_DEV int key_tiles(const Item &t) const {
-    return t.n > 0 && t.hi > t.lo ? (t.hi + bkv - 1) / bkv - first_tile(t) : 0;
+    return t.n > 0 && t.hi > t.lo ? (t.hi + BKV - 1) / BKV - first_tile(t) : 0;
   }
   CRF_DEV int chunks(const Item &t) const { return chunk > 0 ? (key_tiles(t) + chunk - 1) / chunk : 0; }
   CRF_DEV int tile_units(const Item &t) const {
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
   if (tid == 0) bad = 0;
   if (tid < BM) token_pos[tid] = -1;
   stage_groups();
-  Plan plan{p, BKV, G};
+  Plan<BKV> plan{p, G};
   Item it = item_of(p, gr, tid, my_row0, my_n, my_len);
   {
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);

@@ -115,6 +115,26 @@ def test_heads_of_zeros_huge_and_no_numbers(dtype):
     assert torch.isnan(got[1, 1]).any() and ctx.device_errors() == 0
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_without_eps(dtype):
+    """rms_eps 0: a head's norm does not depend on its size, down to values whose squares fp32 does not hold."""
+    import paper_2609_30884_amd as crf
+    from tests.paged import Batch, assert_within
+    from tests.serving import normed, rotated
+    print(f"[case] norm without eps {dtype}", flush=True)
+    b = Batch([(4, 3)], 6, 2, 64, dtype, seed=5)
+    dims = crf.make_dims(2, 128 if dtype == BF else 64, 6, 2, 64, 64, rms_eps=0.0, dtype="bf16" if dtype == BF else "f32")
+    ctx, freq = crf.Context(dims, 1, 0), [1e4 ** (-2 * i / 64) for i in range(32)]
+    q, k, v, (gq, gk) = _inputs(b)
+    q = (q.float() * torch.tensor([1.0, 1e-18, 1e-25, 1e-30, 1e18, 1e30], device="cuda")[:, None]).to(dtype)
+    out = torch.zeros_like(q)
+    crf.norm_rope_append(ctx, crf.rope(64, 1e4), b.batch, q, k, v, gq, gk, b.pool, 1, out)
+    torch.cuda.synchronize()
+    ref, bound = rotated(*normed(q, gq, 0.0), freq, torch.arange(3, 7, device="cuda"), "half", dtype)
+    assert_within(out, ref, bound, "q")
+    assert ctx.device_errors() == 0
+
+
 def test_in_place_bad_pages_and_a_contradicting_sequence():
     import paper_2609_30884_amd as crf
     from tests.paged import Batch, context
