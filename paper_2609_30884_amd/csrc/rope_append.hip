@@ -14,8 +14,13 @@
 // 2^27 and 6e-7 at 2^31.  Cosine, sine and the products are formed in 32 bits and the
 // products rounded to the storage type once.
 //
+// With norms, a head x of q and k is x g / sqrt(mean x^2 + eps) before it turns: the squares of
+// a unit are summed in its thread, then over the head's 4, 8 or 16 lanes, all in 32 bits, and the
+// values stay there until the rotated ones are rounded.
+//
 // 16384 tokens of 28 + 2 * 4 heads of 128, bf16: 53 us, 302 MB, 5.7 TB/s (a large copy
-// reaches 5.0); 8 tokens of 12 + 2 * 2: 4.2 us, of which all but the launch is latency.
+// reaches 5.0) when they were just written, 64 us in a row with other such calls, with norms
+// 69; 8 tokens of 12 + 2 * 2: 4.1 and 4.6 us, of which all but the launch is latency.
 #include <algorithm>
 
 #include "paged.hpp"
@@ -221,7 +226,8 @@ void launch(hipStream_t s, const RopeAppend &p) {
   // Four tokens a workgroup once workgroups outnumber what the chip holds many times over:
   // 12 + 2 * 2 heads of 128 in bf16, one token against four, us: 256 rows 4.4 / 5.8, 1024
   // 5.0 / 6.2, 4096 11.0 / 8.6, 16384 32.0 / 22.9; 28 + 2 * 4 heads: 1024 6.3 / 8.8, 2048
-  // 9.8 / 10.7, 4096 17.0 / 14.9, 16384 65.9 / 53.1.
+  // 9.8 / 10.7, 4096 17.0 / 14.9, 16384 65.9 / 53.1.  With norms, 28 + 2 * 4 heads: 64 rows
+  // 5.0 / 8.6, 2048 13.4 / 13.4, 4096 21.5 / 17.4, 16384 88.8 / 68.9.
   if (n > 2048)
     hipLaunchKernelGGL((rope_append_kernel<T, 4, NORM>), dim3(std::min((n + 3) / 4, MOST_GROUPS)), dim3(NT), 0, s, p);
   else

@@ -9,8 +9,21 @@
 // new tokens of all its sequences (neighbours among the rows) on the rows, or a sequence's
 // own keys with its own new tokens; a unit is a tile of 128 rows of one KV head of an item
 // and a chunk of its keys.  The chunk's length follows from all the items, which every
-// workgroup works out from the lengths on the device: as many units as workgroups stay
-// resident.  The second joins each row's parts, in the order of the keys.
+// workgroup works out from the lengths on the device, an item a thread.  A row sees the keys up
+// to its own position, also among the shared ones, so that a group whose sequences are shorter
+// than it says is right all the same.  The second launch joins each row's parts, in the order
+// of the keys.
+//
+// Measured (bf16, heads of 128), against each sequence reading the shared keys itself:
+//   64 next tokens, four documents of 4096 to 16384 with 16 sequences each, 20 to 500 keys of
+//     their own, 28/4 heads    48 us against 167: 4.4 us until a workgroup knows its unit, 4.5
+//     until its first keys are there, 24 for 118 MB (4.9 TB/s), 3 to store the parts, 8 for
+//     the second launch;
+//   32 about one of 16384    33 us against 83;
+//   four about one of 16384    28 against 36: the same chain.
+// Tried: four stages of 32 keys instead of two of 64, 51 us instead of 48; parts stored whole
+// rows at a time by way of LDS, 54; a body for up to 32 rows whose keys the waves share out,
+// 55 (it spills); a chunk chosen so that one round of workgroups just holds all units, 50.
 #include <math.h>
 
 #include <algorithm>
@@ -162,7 +175,9 @@ struct Plan {
     if (k > 0) sum = make_float4(sum.x + tiles * k, sum.y + tiles, sum.z + rows, sum.w + rows * k);
   }
   // The chunk's length: as many units as half of the workgroups that stay resident (the
-  // sequences' own come on top), and parts for which there is room: an item of k tiles has
+  // sequences' own come on top; with 0.35 / 0.5 / 0.75 of them the 64 above take 51.5 / 48.3 /
+  // 55.2 us, the 32 35 / 33.6 / 37, 64 over 2000 with up to 1000 of their own 41.6 / 37.4 / 33),
+  // and parts for which there is room: an item of k tiles has
   // k / c + 1 parts at most.  (Rounded sums: 2^-10 to spare.)
   CRF_DEV void choose(float4 sum) {
     const float spare = p.part_rows - sum.z * (1.f + 0x1p-10f);

@@ -4,8 +4,10 @@
 //   H = ln S - (sum e^(z - m) (z - m)) / S   (every term of the sum has one sign),
 // and the k largest z by (value, lowest index).
 //
-// One pass over the logits, which is what bounds it: HBM, or for few rows a chain of
-// latencies.  A thread keeps the maximum so far and its two sums, rescaled where a batch of
+// One pass over the logits, which is what bounds it: HBM (2048 rows of 152064 in bf16 124 us,
+// 5.0 TB/s), or for few rows a chain of latencies (one row in fp32 5.2 us, with 5 alternatives
+// 9.5: launch, loads, sums, the parts' stores, ticket and loads, and the alternatives' order; a
+// row that one workgroup takes 3.3 and 5.3).  A thread keeps the maximum so far and its two sums, rescaled where a batch of
 // its loads brings a larger value; a row goes to several workgroups where rows are few, and
 // the last of them to finish joins the parts, in their order.  Sums are fp32.
 //
@@ -13,9 +15,12 @@
 // in its order as an integer, then the lowest index) that exceed a threshold, of which at
 // least k are known to reach it: at first the k-th largest of its lanes' first maxima, later
 // the k-th largest of the list, taken whenever the list runs full.  Later elements of a wave
-// have larger indices, so that only larger values can still enter, and a step costs one
-// comparison an element.  The waves' lists, then the parts', are joined by counting for each
-// key how many are larger.
+// have larger indices, so that only larger values can still enter, and a load costs one
+// comparison: the few that hold a larger value are put side by side in LDS, and the lanes offer
+// their elements to the list.  The waves' lists, then the parts', are joined by counting for
+// each key how many are larger.  (64 rows with 20 alternatives: 39 us when every wave had a
+// threshold of its own and inserted from registers, 20 when the parts were read through the
+// caches after an acquire, 16.6 so; 1024 rows 184 and 75.)
 #include <float.h>
 #include <math.h>
 
@@ -27,12 +32,19 @@ namespace crf {
 namespace {
 
 constexpr int NT = 256, NW = NT / 64;
-constexpr int BATCH = 4;                    // 16-byte loads of a thread in flight
-constexpr int LIST = 128;                   // keys of a wave: k, and one to a lane
+// 16-byte loads of a thread in flight.  8: 2048 rows of 152064 in bf16 119 us instead of 124, but
+// 2048 rows of 2000 with 5 alternatives 24 instead of 14 (registers).
+constexpr int BATCH = 4;
+constexpr int LIST = 128;  // keys of a wave: k, and one to a lane
 static_assert(LOGP_MAX_TOP + 64 <= LIST, "keys");
 constexpr float LOG2E = 1.4426950408889634f;
-// Workgroups that a row is shared out to: until there are FILL of them, none smaller than
-// SMALLEST loads of 16 bytes.
+// Workgroups that a row is shared out to: until there are FILL of them, none with fewer than
+// SMALLEST loads of 16 bytes, and no row that one workgroup has in flight at once.  us with
+// FILL 256 / 512 / 1024 / 2048: 64 rows of 152064 in bf16 with 20 alternatives 18.4 / 16.6 / 18.3
+// / 24.4, without 10.1 / 10.0 / 12.4 / 15.9, 256 rows 34 / 32 / 31 / 38, 300 rows of 32000 14.4 /
+// 16.6 / 19.3 / 28.  SMALLEST 256 / 512 / 1024: a row of 152064 in fp32 with 5 alternatives 9.5 /
+// 9.5 / 10.5, of 32000 10.3 / 9.1 / 9.3; a row of 2000 shared by two 8.5, by none 5.3; four of
+// 8000 in bf16 by two 10.1, by none 6.1.
 constexpr int FILL = 512, SMALLEST = 512;
 
 typedef unsigned long long Key;  // order of the value, ~index; 0: none
@@ -210,6 +222,8 @@ struct Part {
   }
 };
 
+// (Four workgroups a CU: 1024 rows with 20 alternatives 77 us, with the 136 registers of three
+// 81; five spill: 88.)
 template <typename T, bool TOP>
 __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogprobs p, int parts, int each) {
   constexpr int E = Elements<T>::N;
@@ -409,6 +423,8 @@ __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogpro
       __syncthreads();
       // (the parts are read past the caches, as they were written: no line of them is in one)
       if (!last) continue;
+      all = Part{p, row * parts + min(lane, parts - 1)}.sums();
+      if (lane >= parts) all.s = all.w = 0.f;
       if (TOP) {  // (at most a quarter of LOGP_PARTS parts to a wave)
         const int q = (parts + NW - 1) / NW, first = wave * q, keys_held = max(0, min(q, parts - first)) * k;
         constexpr int PER = (LOGP_PARTS / NW * LOGP_MAX_TOP + 63) / 64;
@@ -434,8 +450,6 @@ __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogpro
         for (int c = 0; c < keys_held; c += 64) offer(mine[c + lane], mine[c + lane] >= least);
         join_waves(n);
       }
-      all = Part{p, row * parts + min(lane, parts - 1)}.sums();
-      if (lane >= parts) all.s = all.w = 0.f;
       all.wave();
     }
 
@@ -471,7 +485,8 @@ hipError_t launch(hipStream_t s, const TokenLogprobs &p) {
   const int64_t room = p.n_rows <= p.n_tickets ? p.part_floats / 2 / (2 + LOGP_MAX_TOP) / p.n_rows : 1;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>({(FILL + p.n_rows - 1) / p.n_rows, LOGP_PARTS, room}));
   // (whole steps of a workgroup to a part)
-  const int64_t each = std::max<int64_t>(((loads + most - 1) / most + NT - 1) / NT * NT, SMALLEST);
+  const int64_t least = loads <= BATCH * NT ? BATCH * NT : SMALLEST;
+  const int64_t each = std::max<int64_t>(((loads + most - 1) / most + NT - 1) / NT * NT, least);
   const int64_t parts = std::max<int64_t>(1, (loads + each - 1) / each), units = parts * p.n_rows;
   const dim3 grid((unsigned)std::min<int64_t>(units, LOGP_MOST_GROUPS));
   if (p.top > 0)
