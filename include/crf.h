@@ -134,9 +134,9 @@ int32_t crf_abi_version(void);
  * (head_dim+4), 35 MB at head_dim 128), K-split LoRA partials and, when max_lora_rank > 0, the down projection's
  * adapter sums formed inside the gate/up projection (4 x 2 x 256 x 16 floats
  * per compute unit, 32 MiB on 256 CUs, plus one int per gate/up tile), and 2 KiB
- * of arrival counters.  An fp32 context holds 64 MiB of partials for
- * crf_paged_attention (a bf16 one uses the K-parts' scratch), and every context
- * 21 KiB of counters for the operators over a page pool.  All of
+ * of arrival counters.  An fp32 context holds 64 MiB of partials for attention over
+ * pages and crf_token_logprobs (a bf16 one uses the K-parts' scratch), and every
+ * context 21 KiB of counters for the operators over a page pool.  All of
  * it is freed by crf_context_destroy.  On success *out
  * receives the context.  Errors: INVALID_ARG (null), UNSUPPORTED (see
  * crf_validate_dims), HIP (allocation failed). */
@@ -466,9 +466,11 @@ typedef struct {
 /* crf_paged_attention (without a window) of a batch in groups, whose shared keys and
  * values are read once for all of a group's new tokens.  The same attention, in other
  * last bits; the same to the bit for every call with the same inputs.  It pays where
- * sequences bring few tokens each; a batch whose sequences may bring more than 128 /
- * (n_q_heads/n_kv_heads) (max_new), with more than 1023 groups, or whose parts the context's workspace
- * does not hold, is computed by crf_paged_attention's kernels, which do not look at the
+ * many bring few tokens each over long prefixes.  A batch whose sequences read at most
+ * 40 MB by themselves (as n_seqs and max_pages bound it), may bring more than 128 /
+ * (n_q_heads/n_kv_heads) tokens each (max_new), or come in more than 1023 groups, or
+ * whose parts the context's workspace does not hold (a quarter of it to all rows and
+ * query heads), is computed by crf_paged_attention's kernels, which do not look at the
  * groups.
  * Errors: as crf_paged_attention, SHAPE also for more groups than sequences. */
 crf_status crf_shared_attention(crf_context *ctx, const crf_seq_batch *batch, const crf_seq_groups *groups,
