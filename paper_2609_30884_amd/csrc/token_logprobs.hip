@@ -4,12 +4,13 @@
 //   H = ln S - (sum e^(z - m) (z - m)) / S   (every term of the sum has one sign),
 // and the k largest z by (value, lowest index).
 //
-// One pass over the logits, which is what bounds it: HBM (2048 rows of 152064 in bf16 124 us,
-// 5.0 TB/s), or for few rows a chain of latencies (one row in fp32 5.2 us, with 5 alternatives
-// 9.5: launch, loads, sums, the parts' stores, ticket and loads, and the alternatives' order; a
-// row that one workgroup takes 3.3 and 5.3).  A thread keeps the maximum so far and its two sums, rescaled where a batch of
-// its loads brings a larger value; a row goes to several workgroups where rows are few, and
-// the last of them to finish joins the parts, in their order.  Sums are fp32.
+// One pass over the logits, which is what bounds it: HBM (2048 rows of 152064 in bf16 117 us, 5.3
+// TB/s), or for few rows a chain of latencies (one row in fp32 5.0 us, with 5 alternatives 8.8:
+// launch, loads, sums, the parts' stores, ticket and loads, and the alternatives' order; a row
+// that one workgroup takes 3.2 and 5.2).  A thread keeps the maximum so far and its two sums,
+// rescaled where a batch of its loads brings a larger value; a row goes to several workgroups
+// where rows are few, and the last of them to finish joins the parts, in their order.  Sums are
+// fp32.
 //
 // The most likely tokens are found on the way.  A wave keeps a list in LDS of the keys (value
 // in its order as an integer, then the lowest index) that exceed a threshold, of which at
@@ -20,7 +21,7 @@
 // their elements to the list.  The waves' lists, then the parts', are joined by counting for
 // each key how many are larger.  (64 rows with 20 alternatives: 39 us when every wave had a
 // threshold of its own and inserted from registers, 20 when the parts were read through the
-// caches after an acquire, 16.6 so; 1024 rows 184 and 75.)
+// caches after an acquire, 15.7 so; 1024 rows 184 and 73.)
 #include <float.h>
 #include <math.h>
 
@@ -32,7 +33,7 @@ namespace crf {
 namespace {
 
 constexpr int NT = 256, NW = NT / 64;
-// 16-byte loads of a thread in flight.  8: 2048 rows of 152064 in bf16 119 us instead of 124, but
+// 16-byte loads of a thread in flight.  8: 2048 rows of 152064 in bf16 114 us instead of 117, but
 // 2048 rows of 2000 with 5 alternatives 24 instead of 14 (registers).
 constexpr int BATCH = 4;
 constexpr int LIST = 128;  // keys of a wave: k, and one to a lane
@@ -40,11 +41,11 @@ static_assert(LOGP_MAX_TOP + 64 <= LIST, "keys");
 constexpr float LOG2E = 1.4426950408889634f;
 // Workgroups that a row is shared out to: until there are FILL of them, none with fewer than
 // SMALLEST loads of 16 bytes, and no row that one workgroup has in flight at once.  us with
-// FILL 256 / 512 / 1024 / 2048: 64 rows of 152064 in bf16 with 20 alternatives 18.4 / 16.6 / 18.3
-// / 24.4, without 10.1 / 10.0 / 12.4 / 15.9, 256 rows 34 / 32 / 31 / 38, 300 rows of 32000 14.4 /
-// 16.6 / 19.3 / 28.  SMALLEST 256 / 512 / 1024: a row of 152064 in fp32 with 5 alternatives 9.5 /
-// 9.5 / 10.5, of 32000 10.3 / 9.1 / 9.3; a row of 2000 shared by two 8.5, by none 5.3; four of
-// 8000 in bf16 by two 10.1, by none 6.1.
+// FILL 256 / 512 / 1024 / 2048: 64 rows of 152064 in bf16 with 20 alternatives 17.4 / 15.7 / 17.2
+// / 23.5, without 9.9 / 9.8 / 12.3 / 15.7, 256 rows 33 / 31 / 29 / 36, 300 rows of 32000 14.0 /
+// 15.6 / 18.5 / 26.  SMALLEST 256 / 512 / 1024: a row of 152064 in fp32 with 5 alternatives 8.8 /
+// 8.8 / 9.4, of 32000 9.1 / 8.1 / 8.3; a row of 2000 shared by two 7.6, by none 5.2; four of
+// 8000 in bf16 by two 9.1, by none 6.0.
 constexpr int FILL = 512, SMALLEST = 512;
 
 typedef unsigned long long Key;  // order of the value, ~index; 0: none
@@ -68,12 +69,13 @@ CRF_DEV void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The largest number of the leading BITS bits that at least k of the lanes' values reach.
-template <int BITS>
+// The largest number of the leading 16 bits that at least k of the lanes' values reach: all the
+// bits that bf16 has, and for fp32 a bound that lets few more in (with all 32: 8 rows of 152064
+// in bf16 with 20 alternatives 14.6 us instead of 13.0, a row in fp32 with 5 9.5 and 8.8).
 CRF_DEV uint32_t reached_by(uint32_t v, int k) {
   uint32_t least = 0;
 #pragma unroll 4
-  for (int b = 31; b > 31 - BITS; --b) {
+  for (int b = 31; b >= 16; --b) {
     const uint32_t more = least | 1u << b;
     if (__popcll(__builtin_amdgcn_ballot_w64(v >= more)) >= k) least = more;
   }
@@ -88,12 +90,12 @@ CRF_DEV int place(Key own, lds_key *keys, int n) {
   wave_order();
   int rank = 0;
 #pragma unroll 1
-  for (int l = 0; l < n; l += 8) {
-    Key other[8];
+  for (int l = 0; l < n; l += 16) {
+    Key other[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) other[i] = keys[l + i];
+    for (int i = 0; i < 16; ++i) other[i] = keys[l + i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rank += other[i] > own;
+    for (int i = 0; i < 16; ++i) rank += other[i] > own;
   }
   wave_order();
   return rank;
@@ -107,7 +109,7 @@ CRF_DEV int keep_largest(lds_key *list, int n, int k) {
   wave_order();
   if (n > 64) {
     // a value that k of the lanes' larger ones reach: no key below it is one of the k
-    const Key least = (Key)reached_by<32>((uint32_t)((a > b ? a : b) >> 32), k) << 32;
+    const Key least = (Key)reached_by((uint32_t)((a > b ? a : b) >> 32), k) << 32;
     const uint64_t ma = __builtin_amdgcn_ballot_w64(a >= least && a), mb = __builtin_amdgcn_ballot_w64(b >= least && b);
     const int na = __popcll(ma), both = na + __popcll(mb);
     if (both <= 64) {
@@ -222,8 +224,8 @@ struct Part {
   }
 };
 
-// (Four workgroups a CU: 1024 rows with 20 alternatives 77 us, with the 136 registers of three
-// 81; five spill: 88.)
+// (Four workgroups a CU: 1024 rows with 20 alternatives 73 us, with the 136 registers of three
+// 77; five spill: 87.)
 template <typename T, bool TOP>
 __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogprobs p, int parts, int each) {
   constexpr int E = Elements<T>::N;
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogpro
       }
       if constexpr (TOP) {
         if (a == l0) {  // a value that k of the workgroup's lanes' maxima reach
-          uint32_t o = least_of_waves(reached_by<16>(order(most), quarter)) - 1;
+          uint32_t o = least_of_waves(reached_by(order(most), quarter)) - 1;
           if (o == 0x7fffffffu) --o;  // (zero's own place below is -0, which equals it)
           above = value(o);
         }
@@ -392,8 +394,9 @@ __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogpro
       }
     }
     // the elements before and behind the loads: at most one a lane
-    if (wave == 0) {
-      const int tail = head + loads * E, i = lane < E ? lane : tail + lane - E;
+    const int tail = head + loads * E;
+    if (wave == 0 && ((part == 0 && head > 0) || (part == parts - 1 && tail < V))) {
+      const int i = lane < E ? lane : tail + lane - E;
       const bool mine = lane < E ? part == 0 && i < head : part == parts - 1 && i < V;
       const float v = mine ? at(z, i) : -INFINITY;
       if (v > sum.m) sum.to(v);
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(NT, 4) void token_logprobs_kernel(const TokenLogpro
           most = max(most, (uint32_t)(keys[i] >> 32));
           mine[i * 64 + lane] = keys[i];
         }
-        const Key least = (Key)max(1u, least_of_waves(reached_by<32>(most, quarter))) << 32;
+        const Key least = (Key)max(1u, least_of_waves(reached_by(most, quarter))) << 32;
         n = 0;
 #pragma unroll 1
         for (int c = 0; c < keys_held; c += 64) offer(mine[c + lane], mine[c + lane] >= least);

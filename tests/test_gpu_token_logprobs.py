@@ -139,6 +139,21 @@ def test_orders_and_ties(dtype, top):
     _check(z.repeat(150, 1), tokens.repeat(150, 1), top, "whole rows")
 
 
+@pytest.mark.parametrize("top", [1, 20, 32])
+def test_values_that_differ_in_their_last_bits(top):
+    """All values of a row have the same leading 16 bits, which bound what may be among the largest."""
+    print(f"[case] logprobs last bits top {top}", flush=True)
+    v = 30011
+    g = torch.Generator(device="cuda").manual_seed(8)
+    up = 1 + torch.arange(v, device="cuda") * 2.0**-23
+    shuffled = up[torch.randperm(v, generator=g, device="cuda")]
+    few = 1 + torch.randint(0, 40, (v,), generator=g, device="cuda") * 2.0**-23
+    z = torch.stack([up, up.flip(0), -up, shuffled, -shuffled, few, -few, 1e30 * shuffled])
+    tokens = torch.tensor([[0, v - 1]] * len(z), dtype=torch.int32, device="cuda")
+    _check(z, tokens, top, "split rows")
+    _check(z.repeat(150, 1), tokens.repeat(150, 1), top, "whole rows")
+
+
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("many", [1, 200])
 def test_values_at_the_ends(dtype, many):
