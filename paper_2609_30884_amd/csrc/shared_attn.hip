@@ -317,7 +317,7 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
       for (int s = u.seq + tid; s < a.b.n_seqs; s += NT) {
         int start, len;
         const int m = seq_new(a.b, s, start, len);
-        if (start >= first + tokens) break;
+        if (m > 0 && start >= first + tokens) break;  // (one that contradicts the batch has no rows, wherever they start)
         place(start, m, len);
       }
     }

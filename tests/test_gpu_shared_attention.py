@@ -168,6 +168,15 @@ def test_groups_that_contradict():
     _check(b, "short first", flags=2)
 
 
+def test_a_contradicting_sequence_among_many():
+    """Row starts out of range in a batch of more sequences than a workgroup has threads: two have no rows, all others
+    of the group are right."""
+    print("[case] shared contradiction among many", flush=True)
+    b = Grouped([(40, [(1, i % 5) for i in range(600)])], 4, 2, 64, BF, seed=18, pad=2, max_new=1)
+    b.row_start[10] = 1 << 30
+    _check(b, "row start out of range", flags=2, skip=[9, 10])
+
+
 def test_rows_claimed_over_and_over():
     """Row starts that go back and forth claim more rows than there are: flagged, and no row is written out of range."""
     import paper_2609_30884_amd as crf
