@@ -175,8 +175,9 @@ struct Plan {
     if (k > 0) sum = make_float4(sum.x + tiles * k, sum.y + tiles, sum.z + rows, sum.w + rows * k);
   }
   // The chunk's length: as many units as half of the workgroups that stay resident (the
-  // sequences' own come on top; with 0.35 / 0.5 / 0.75 of them the 64 above take 51.5 / 48.3 /
-  // 55.2 us, the 32 35 / 33.6 / 37, 64 over 2000 with up to 1000 of their own 41.6 / 37.4 / 33),
+  // sequences' own come on top; with 0.35 / 0.5 / 0.62 / 0.75 of them the 64 above take 52.0 /
+  // 48.5 / 47.6 / 55.5 us, the 32 35.1 / 32.9 / 33.3 / 38.0, two times eight drafts of 8 over 8192
+  // 48.4 / 45.2 / 47.5 / 44.8, 64 over 2000 with up to 1000 of their own 36.3 / 32.7 / 30.8 / 32.8),
   // and parts for which there is room: an item of k tiles has
   // k / c + 1 parts at most.  (Rounded sums: 2^-10 to spare.)
   CRF_DEV void choose(float4 sum) {
@@ -273,11 +274,17 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
     }
     return units;
   };
-  const int units = scan((int)blockIdx.x, blockIdx.x == 0);
-  // The units, of which the first (the groups') are the longest, are dealt out back and forth.
+  // The units, of which the first (the groups') are the longest, are dealt out back and forth.  The
+  // first half of the workgroups, one to a CU, begins with its last unit, so that those which
+  // share a CU with one of the second half are the ones with short units (otherwise 64 sequences
+  // over 2000 tokens with up to 1000 of their own, 28/4 heads, 37.4 us instead of 32.8, 48 over
+  // eight documents, 12/2, 27.7 instead of 25.8; two times eight drafts 45.2 instead of 45.6).
+  const int wg = (int)blockIdx.x, half = (int)gridDim.x / 2;
+  const int begin = wg < half ? half - 1 - wg : wg;
+  const int units = scan(begin, wg == 0);
 #pragma unroll 1
   for (int round = 0;; ++round) {
-    const int nth = round * (int)gridDim.x + (round % 2 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    const int nth = round * (int)gridDim.x + (round % 2 ? (int)gridDim.x - 1 - begin : begin);
     if (nth >= units) break;
     if (round > 0) {  // (the items are worked out again: kept, their registers would be spilled)
       __syncthreads();  // (the unit before has left LDS)
