@@ -5,7 +5,7 @@
 // and the k largest z by (value, lowest index).
 //
 // One pass over the logits, which is what bounds it: HBM (2048 rows of 152064 in bf16 117 us, 5.3
-// TB/s), or for few rows a chain of latencies (one row in fp32 5.0 us, with 5 alternatives 8.8:
+// TB/s), or for few rows a chain of latencies (one row in fp32 5.0 us, with 5 alternatives 8.6:
 // launch, loads, sums, the parts' stores, ticket and loads, and the alternatives' order; a row
 // that one workgroup takes 3.2 and 5.2).  A thread keeps the maximum so far and its two sums,
 // rescaled where a batch of its loads brings a larger value; a row goes to several workgroups
@@ -21,7 +21,7 @@
 // their elements to the list.  The waves' lists, then the parts', are joined by counting for
 // each key how many are larger.  (64 rows with 20 alternatives: 39 us when every wave had a
 // threshold of its own and inserted from registers, 20 when the parts were read through the
-// caches after an acquire, 15.7 so; 1024 rows 184 and 73.)
+// caches after an acquire, 15.5 so; 1024 rows 184 and 73.)
 #include <float.h>
 #include <math.h>
 
@@ -71,10 +71,11 @@ CRF_DEV void wave_order() {
 
 // The largest number of the leading 16 bits that at least k of the lanes' values reach: all the
 // bits that bf16 has, and for fp32 a bound that lets few more in (with all 32: 8 rows of 152064
-// in bf16 with 20 alternatives 14.6 us instead of 13.0, a row in fp32 with 5 9.5 and 8.8).
+// in bf16 with 20 alternatives 14.6 us instead of 13.0, a row in fp32 with 5 9.5 and 8.8; written
+// out 12.7 and 8.6, as a loop 13.5 and 9.1; two bits a step, three counts each, 13.0 and 8.7).
 CRF_DEV uint32_t reached_by(uint32_t v, int k) {
   uint32_t least = 0;
-#pragma unroll 4
+#pragma unroll
   for (int b = 31; b >= 16; --b) {
     const uint32_t more = least | 1u << b;
     if (__popcll(__builtin_amdgcn_ballot_w64(v >= more)) >= k) least = more;
