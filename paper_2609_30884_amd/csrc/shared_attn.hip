@@ -428,20 +428,26 @@ __global__ __launch_bounds__(NT) void shared_join_kernel(const SharedAttn p) {
   const PagedAttn &a = p.a;
   const int tid = threadIdx.x, G = a.nq / a.nkv, e = 4 * (tid % LANES);
   const Info *info = (const Info *)p.info;
-  __shared__ Info found;
+  __shared__ int owner;
 #pragma unroll 1
   for (int64_t unit = blockIdx.x; unit < (int64_t)a.b.n_rows * a.nkv; unit += gridDim.x) {
     const int token = (int)(unit / a.nkv), kvh = (int)(unit - (int64_t)token * a.nkv);
     __syncthreads();
-    if (tid == 0) found.own.n = 0;
+    if (tid == 0) owner = -1;
     __syncthreads();
+    // Where row starts descend, several sequences may claim the token: it is the last one's.  (Their
+    // Infos stored to one place could come out as a mixture, which names parts that nobody has
+    // laid out.)
+    int claims = -1;
     for (int s = tid; s < a.b.n_seqs; s += NT) {
-      const Info f = info[s];
-      if (token >= f.own.row0 && token < f.own.row0 + f.own.n) found = f;
+      const int row0 = info[s].own.row0, n = info[s].own.n;
+      if (token >= row0 && token < row0 + n) claims = s;
     }
+    if (claims >= 0) atomicMax(&owner, claims);
     __syncthreads();
-    const Info f = found;
-    if (f.own.n == 0) continue;  // a row of nobody
+    const int whose = __builtin_amdgcn_readfirstlane(owner);
+    if (whose < 0) continue;  // a row of nobody
+    const Info f = info[whose];
     const int parts = f.shared.chunks + f.own.chunks;
     for (int r = tid / LANES; r < G; r += ROWS) {
       auto slot = [&](int j) {
