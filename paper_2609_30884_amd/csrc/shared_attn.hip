@@ -192,6 +192,7 @@ struct Plan {
 
 struct Unit {
   int row0, n, lo, hi, seq;  // of the item
+  int until;                 // its sequences: seq .. until - 1
   int base, number;          // first row of its parts, and which of its units this is
 };
 
@@ -256,7 +257,10 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
         units += ends[w].x;
         part_rows += ends[w].y;
       }
-      if (u >= from && u < from + num) unit = Unit{it.row0, it.n, it.lo, it.hi, it.seq, base, u - from};
+      if (u >= from && u < from + num) {
+        const int i = i0 + tid, until = i < p.n_groups ? gr.start[i + 1] : it.seq + 1;
+        unit = Unit{it.row0, it.n, it.lo, it.hi, it.seq, until, base, u - from};
+      }
       if (write) {  // (the groups lie before the sequences)
         const int i = i0 + tid, chunks = plan.chunks(it);
         if (i < p.n_groups) {
@@ -297,8 +301,8 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
     __syncthreads();
     const Unit u{__builtin_amdgcn_readfirstlane(unit.row0), __builtin_amdgcn_readfirstlane(unit.n),
                  __builtin_amdgcn_readfirstlane(unit.lo),   __builtin_amdgcn_readfirstlane(unit.hi),
-                 __builtin_amdgcn_readfirstlane(unit.seq),  __builtin_amdgcn_readfirstlane(unit.base),
-                 __builtin_amdgcn_readfirstlane(unit.number)};
+                 __builtin_amdgcn_readfirstlane(unit.seq),  __builtin_amdgcn_readfirstlane(unit.until),
+                 __builtin_amdgcn_readfirstlane(unit.base), __builtin_amdgcn_readfirstlane(unit.number)};
     const int n = u.n, lo = u.lo, hi = u.hi;
     const Item item{u.row0, n, lo, hi, u.seq, -1};
     const int each = plan.tile_units(item), tile = u.number / each, x = u.number - tile * each;
@@ -313,18 +317,18 @@ __global__ __launch_bounds__(NT, 2) void shared_parts_kernel(const SharedAttn p)
     const int tok = row / G, head = kvh * G + row - tok * G;
     QFrag<T, HD> q;
     q.load((const T *)a.q + (int64_t)(u.row0 + tok) * a.q_ld + head * HD, g);
-    // positions of the tile's tokens (-1: of no sequence)
+    // positions of the tile's tokens in the item's sequences (-1: in none; the largest where row
+    // starts descend and several claim a token: no matter which comes first)
     auto place = [&](int start, int m, int len) {
       for (int t = max(start, first); t < min(start + m, first + tokens); ++t)
-        token_pos[t - first] = len - m + t - start;
+        atomicMax(&token_pos[t - first], len - m + t - start);
     };
     if (one) {
-      if (tid >= p.n_groups && it.n > 0) place(it.row0, it.n, it.hi);
+      if (tid >= p.n_groups && it.n > 0 && it.seq >= u.seq && it.seq < u.until) place(it.row0, it.n, it.hi);
     } else {
-      for (int s = u.seq + tid; s < a.b.n_seqs; s += NT) {
+      for (int s = u.seq + tid; s < u.until; s += NT) {
         int start, len;
         const int m = seq_new(a.b, s, start, len);
-        if (m > 0 && start >= first + tokens) break;  // (one that contradicts the batch has no rows, wherever they start)
         place(start, m, len);
       }
     }
