@@ -153,11 +153,15 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
     const int upr = half / E;                     // rotated units of a head
     const int uph = p.hd / (2 * E);               // units of a head
     // (uph is 4, 8 or 16: a thread has the same unit of all its heads)
-    const int u = tid % uph, step = NT / uph, heads = p.nq + 2 * p.nkv;
+    const int lg = __builtin_ctz(uph), u = tid & (uph - 1), step = NT >> lg, heads = p.nq + 2 * p.nkv;
     int j = 0;  // the token, of which the thread's head is h
-    for (int h = tid / uph;; h += step) {
-      while (h >= heads) h -= heads, ++j;
-      if (j >= TPW) break;
+    for (int h = tid >> lg;; h += step) {
+      if constexpr (TPW == 1) {
+        if (h >= heads) break;
+      } else {
+        while (h >= heads) h -= heads, ++j;
+        if (j >= TPW) break;
+      }
       if (pos_s[j] < 0) continue;
       const int64_t row = row0 + j;
       const T *src;
