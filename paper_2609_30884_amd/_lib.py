@@ -440,6 +440,17 @@ def _int32(t, n: Optional[int], name: str):
     return t
 
 
+def _to_int32(n: int) -> int:
+    """ctypes would take an int's low 32 bits; past the longest sequence a number of keys is all of them."""
+    return max(-1, min(n, 0x7fffffff))
+
+
+def _counts(*ns):
+    """Counts that an int holds (ctypes would take the others' low 32 bits)."""
+    if max(ns) > 0x7fffffff:
+        raise CrfError(2, f"a count of {max(ns)} passes 32 bits")
+
+
 def _tables(t):
     import torch
     if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or \
@@ -496,7 +507,8 @@ def seq_batch(row_start, length, block_tables, n_rows: int, max_new: int = 0) ->
     paged_attention chooses its kernel by: a batch of single tokens should pass max_new=1."""
     t = _tables(block_tables)
     n = t.shape[0]
-    b = SeqBatch(n, int(n_rows), int(max_new), t.shape[1], t.stride(0) if n > 1 else t.shape[1],
+    _counts(n, int(n_rows), t.shape[1])
+    b = SeqBatch(n, int(n_rows), _to_int32(int(max_new)), t.shape[1], t.stride(0) if n > 1 else t.shape[1],
                  _int32(row_start, n + 1, "row_start").data_ptr(), _int32(length, n, "length").data_ptr(), t.data_ptr())
     b.tensors, b.device = (row_start, length, block_tables), _same_device(row_start, length, block_tables)
     return b
@@ -572,11 +584,6 @@ def _attention_rows(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int
     return rows
 
 
-def _to_int32(n: int) -> int:
-    """ctypes would take an int's low 32 bits; past the longest sequence a number of keys is all of them."""
-    return max(-1, min(n, 0x7fffffff))
-
-
 def paged_attention(ctx: Context, batch: SeqBatch, q, pool: PagePool, layer: int, out, lse=None, scale: float = 0.0,
                     window: int = 0, stream=None):
     """crf_paged_attention: out [rows, heads, head_dim] (and lse, fp32 [rows, heads]) of the new tokens' queries q."""
@@ -599,6 +606,7 @@ def seq_groups(seq_start, shared_len) -> SeqGroups:
     """seq_start [G + 1], shared_len [G]: int32 device tensors; sequences seq_start[g] .. seq_start[g + 1] - 1 of a batch
     share the keys and values of their first shared_len[g] tokens."""
     n = shared_len.numel()
+    _counts(n)
     g = SeqGroups(n, _int32(seq_start, n + 1, "seq_start").data_ptr(), _int32(shared_len, n, "shared_len").data_ptr())
     g.tensors, g.device = (seq_start, shared_len), _same_device(seq_start, shared_len)
     return g
@@ -715,6 +723,7 @@ def token_logprobs(ctx: Context, logits, tokens=None, logprob=None, entropy=None
             raise CrfError(2, f"top_token must be [{rows}, top]")
         top = shape[1]
         kp, vp = _values(top_token, shape, i32, "top_token"), _values(top_logprob, shape, f32, "top_logprob")
+    _counts(rows, vocab, n, top)
     ep, sp = _values(entropy, (rows,), f32, "entropy"), _values(lse, (rows,), f32, "lse")
     _check_device(ctx, (), (logits, tokens, logprob, entropy, lse, top_token, top_logprob))
     st = ctx.lib.crf_token_logprobs(ctx.handle, CRF_F32 if logits.dtype is f32 else CRF_BF16, logits.data_ptr(),
