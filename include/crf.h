@@ -467,11 +467,13 @@ typedef struct {
  * values are read once for all of a group's new tokens.  The same attention, in other
  * last bits; the same to the bit for every call with the same inputs.  It pays where
  * many bring few tokens each over long prefixes.  A batch whose sequences read at most
- * 40 MB by themselves (as n_seqs and max_pages bound it), may bring more than 128 /
- * (n_q_heads/n_kv_heads) tokens each (max_new), or come in more than 1023 groups, or
- * whose parts the context's workspace does not hold (a quarter of it to all rows and
- * query heads), is computed by crf_paged_attention's kernels, which do not look at the
- * groups.
+ * 40 MB by themselves (as n_seqs and max_pages bound it), of which one may bring more
+ * than 128 / (n_q_heads/n_kv_heads) tokens (max_new), or that comes in more than 1023
+ * groups, or whose parts the context's workspace does not hold (a quarter of it to all
+ * rows and query heads), is computed by crf_paged_attention's kernels, which do not look
+ * at the groups: one long chunk among single tokens ends sharing for all of them.  With
+ * max_new 0, a batch of up to two rows a sequence on average is taken for one of short
+ * sequences, any other for one that may bring long ones.
  * Errors: as crf_paged_attention, SHAPE also for more groups than sequences. */
 crf_status crf_shared_attention(crf_context *ctx, const crf_seq_batch *batch, const crf_seq_groups *groups,
                                 const void *q, int64_t q_stride, const crf_page_pool *pool, int32_t layer, float scale,

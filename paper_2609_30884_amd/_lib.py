@@ -614,7 +614,8 @@ def seq_groups(seq_start, shared_len) -> SeqGroups:
 
 def shared_attention(ctx: Context, batch: SeqBatch, groups: SeqGroups, q, pool: PagePool, layer: int, out, lse=None,
                      scale: float = 0.0, stream=None):
-    """crf_shared_attention: paged_attention of a batch in groups whose shared keys are read once."""
+    """crf_shared_attention: paged_attention of a batch in groups whose shared keys are read once.  A batch whose max_new
+    says that a sequence may bring a long chunk shares nothing; one without max_new shares up to two rows a sequence."""
     qr, outr = _attention_rows(ctx, batch, q, pool, layer, out, lse)
     _check_device(ctx, (groups,), ())
     st = ctx.lib.crf_shared_attention(ctx.handle, batch, groups, *qr, pool, layer, scale, *outr, _ptr(lse),

@@ -38,6 +38,7 @@ constexpr int SHARED_MAX_GROUPS = 1023;
 
 struct SharedAttn {
   PagedAttn a;  // the batch (no window)
+  int max_new;   // as the caller bounds it (0: not at all)
   int n_groups;
   const int32_t *seq_start, *shared_len;  // [n_groups + 1], [n_groups]
   // set by the launcher: the items' table, and the parts' O [part_rows][hd] and (reference, sum)

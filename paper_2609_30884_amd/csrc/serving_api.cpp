@@ -67,6 +67,7 @@ crf_status crf_shared_attention(crf_context *ctx, const crf_seq_batch *batch, co
   if (groups->n_groups > 0 && (!groups->seq_start || !groups->shared_len || !aligned4(groups->seq_start) ||
                                !aligned4(groups->shared_len)))
     return fail(ctx, CRF_ERR_INVALID_ARG, "%s: seq_start or shared_len NULL or misaligned", what);
+  p.max_new = batch->max_new;
   p.n_groups = groups->n_groups;
   p.seq_start = groups->seq_start;
   p.shared_len = groups->shared_len;
