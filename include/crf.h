@@ -432,6 +432,8 @@ crf_status crf_paged_attention(crf_context *ctx, const crf_seq_batch *batch, con
  *   q_norm, k_norm: the gains g [head_dim], storage type, 16-byte aligned, one for
  *   all heads of q and of k (q_norm may be NULL where q is).
  * Norm, rotation and products are fp32, rounded to the storage type once.
+ * The windows (crf_recompute_window and its kin) and crf_decode_logits know no norms of
+ * heads: pages written by this call are not theirs to refresh or to decode from.
  * Otherwise as crf_rope_append, its errors included. */
 crf_status crf_norm_rope_append(crf_context *ctx, const crf_rope *rope, const crf_seq_batch *batch,
                                 const int32_t *positions, const void *q, int64_t q_stride, const void *k,
@@ -443,7 +445,8 @@ crf_status crf_norm_rope_append(crf_context *ctx, const crf_rope *rope, const cr
  * row at position p sees the keys j <= p with j > p - window or j < sinks.  Their
  * pages must still be in the block tables; those between need not be, as long as
  * their entries name pages of the pool (what lies there is not seen).  window 0:
- * every key.  Otherwise as crf_paged_attention; with sinks 0 the same to the bit.
+ * every key.  The windows and crf_decode_logits attend to every key, without sinks.
+ * Otherwise as crf_paged_attention; with sinks 0 the same to the bit.
  * Errors: as crf_paged_attention, SHAPE also for negative sinks. */
 crf_status crf_sink_attention(crf_context *ctx, const crf_seq_batch *batch, const void *q, int64_t q_stride,
                               const crf_page_pool *pool, int32_t layer, float scale, int32_t window, int32_t sinks,

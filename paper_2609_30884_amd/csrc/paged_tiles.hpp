@@ -225,6 +225,12 @@ CRF_DEV uint64_t not_finite(const RowState<HD> &st) {
 
 // O += P V for the probabilities p of 32 keys (V rows from vt on).  CAREFUL: bit v of `on`
 // is set where the row sees the key of p[v].
+//
+// In bf16 the probabilities are rounded, to nearest, to the type that the matrix instructions
+// take; their sum is formed before that.  The reference is not the row's maximum, so that the
+// largest weight is rounded too.  Off from 64 bits, of the outputs' RMS, heads of 128 over 16000
+// keys: 0.0023; with a maximum as the reference 0.0020; with probabilities in 32 bits, which need
+// products at an eighth of the rate, 0.0017, the outputs' own rounding.  No part of it is one-sided.
 template <typename T, int HD, Take TAKE>
 CRF_DEV void weigh(const lds_mem *vt, const float (&p)[16], RowState<HD> &st, int lane, uint32_t on_bits = 0) {
   using L = Layout<T, HD>;

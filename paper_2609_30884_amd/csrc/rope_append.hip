@@ -20,7 +20,7 @@
 //
 // 16384 tokens of 28 + 2 * 4 heads of 128, bf16: 53 us, 302 MB, 5.7 TB/s (a large copy
 // reaches 5.0) when they were just written, 64 us in a row with other such calls, with norms
-// 69; 8 tokens of 12 + 2 * 2: 4.1 and 4.6 us, of which all but the launch is latency.
+// 68 to 69; 8 tokens of 12 + 2 * 2: 3.8 and 4.6 us, of which all but the launch is latency.
 #include <algorithm>
 
 #include "paged.hpp"

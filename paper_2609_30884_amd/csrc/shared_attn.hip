@@ -16,14 +16,19 @@
 //
 // Measured (bf16, heads of 128), against each sequence reading the shared keys itself:
 //   64 next tokens, four documents of 4096 to 16384 with 16 sequences each, 20 to 500 keys of
-//     their own, 28/4 heads    48 us against 167: 4.4 us until a workgroup knows its unit, 4.5
-//     until its first keys are there, 24 for 118 MB (4.9 TB/s), 3 to store the parts, 8 for
-//     the second launch;
+//     their own, 28/4 heads    48 us against 171, three batches in turn (one or two, which the
+//     memory-side cache holds, 40): 4.4 us until a workgroup knows its unit, 4.5 until its
+//     first keys are there, 24 for 118 MB (4.9 TB/s), 3 to store the parts, 7 for the second
+//     launch;
 //   32 about one of 16384    33 us against 83;
-//   four about one of 16384    28 against 36: the same chain.
-// Tried: four stages of 32 keys instead of two of 64, 51 us instead of 48; parts stored whole
-// rows at a time by way of LDS, 54; a body for up to 32 rows whose keys the waves share out,
-// 55 (it spills); a chunk chosen so that one round of workgroups just holds all units, 50.
+//   four about one of 16384    28 against 36: the same chain;
+//   two times eight drafts of 8 over 8192    46 against 73: products of full tiles on half of the
+//     workgroups that stay resident (choose() below), 13 at the rate of a large matrix product;
+//   fp32, four times eight next tokens over 3000, 3/1 heads    38 against 50.
+// Tried when the first of these took 48 to 49 us: four stages of 32 keys instead of two of 64, 51;
+// parts stored whole rows at a time by way of LDS, 54; a body for up to 32 rows whose keys the
+// waves share out, 55 (it spills); a chunk chosen so that one round of workgroups just holds all
+// units, 50.
 #include <math.h>
 
 #include <algorithm>

@@ -5,20 +5,23 @@
 // and the k largest z by (value, lowest index).
 //
 // One pass over the logits, which is what bounds it: HBM (2048 rows of 152064 in bf16 117 us, 5.3
-// TB/s), or for few rows a chain of latencies (one row in fp32 5.0 us, with 5 alternatives 8.6:
+// TB/s; streams that are only read reach 5.2 to 5.9 here), or for few rows a chain of latencies (one row in fp32 5.0 us, with 5 alternatives 8.6:
 // launch, loads, sums, the parts' stores, ticket and loads, and the alternatives' order; a row
 // that one workgroup takes 3.2 and 5.2).  A thread keeps the maximum so far and its two sums,
-// rescaled where a batch of its loads brings a larger value; a row goes to several workgroups
+// rescaled where a batch of its loads brings a larger value, to which each batch's terms are
+// added as one sum; a row goes to several workgroups
 // where rows are few, and the last of them to finish joins the parts, in their order.  Sums are
 // fp32.
 //
 // The most likely tokens are found on the way.  A wave keeps a list in LDS of the keys (value
-// in its order as an integer, then the lowest index) that exceed a threshold, of which at
-// least k are known to reach it: at first the k-th largest of its lanes' first maxima, later
-// the k-th largest of the list, taken whenever the list runs full.  Later elements of a wave
-// have larger indices, so that only larger values can still enter, and a load costs one
-// comparison: the few that hold a larger value are put side by side in LDS, and the lanes offer
-// their elements to the list.  The waves' lists, then the parts', are joined by counting for
+// in its order as an integer, then the lowest index) that reach a threshold below which none of
+// the workgroup's k largest lies.  At first it is the same for all four waves: of what a quarter
+// of k of each wave's lanes reach with their first maxima, in the leading 16 bits, the least, so
+// that k lanes of the workgroup reach it, however few of one wave's do.  Whenever a wave's list
+// runs full it is cut to its k largest, and its k-th is that wave's threshold from then on.  Later
+// elements of a wave have larger indices, so that only larger values can still enter, and a load
+// costs one comparison: the few that hold a larger value are put side by side in LDS, and the lanes
+// offer their elements to the list.  The waves' lists, then the parts', are joined by counting for
 // each key how many are larger.  (64 rows with 20 alternatives: 39 us when every wave had a
 // threshold of its own and inserted from registers, 20 when the parts were read through the
 // caches after an acquire, 15.5 so; 1024 rows 184 and 73.)
