@@ -447,8 +447,8 @@ def _to_int32(n: int) -> int:
 
 def _counts(*ns):
     """Counts that an int holds (ctypes would take the others' low 32 bits)."""
-    if max(ns) > 0x7fffffff:
-        raise CrfError(2, f"a count of {max(ns)} passes 32 bits")
+    if max(ns) > 0x7fffffff or min(ns) < -0x7fffffff:
+        raise CrfError(2, f"a count of {max(ns, key=abs)} passes 32 bits")
 
 
 def _tables(t):

@@ -125,7 +125,8 @@ __global__ __launch_bounds__(NT) void rope_append_kernel(const RopeAppend p) {
 #pragma unroll
       for (int j = 0; j < TPW; ++j)
         if (row0 + j >= start && row0 + j < start + n)
-          __hip_atomic_store(&token_s[j], (int64_t)s << 32 | (len - n + row0 + j - start), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          __hip_atomic_store(&token_s[j], (int64_t)s << 32 | (len - n + row0 + j - start), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_WORKGROUP);
     }
     __syncthreads();
     const int half = p.rotary_dim / 2;

@@ -36,7 +36,7 @@ def test_token_logprobs_takes_counts_of_31_bits():
     assert got[0][4:6] == (most, 50)
 
 
-@pytest.mark.parametrize("seqs,pages,rows", [(BIG + 3, 2, 6), (3, BIG + 2, 6), (3, 2, BIG + 6)])
+@pytest.mark.parametrize("seqs,pages,rows", [(BIG + 3, 2, 6), (3, BIG + 2, 6), (3, 2, BIG + 6), (3, 2, 6 - BIG)])
 def test_batches_of_counts_past_32_bits_are_refused(seqs, pages, rows):
     with pytest.raises(crf.CrfError) as e:
         crf.seq_batch(_none(seqs + 1), _none(seqs), _none(seqs, pages), rows)
